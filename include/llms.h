@@ -273,6 +273,73 @@ int llms_compress_context(const llms_kv_desc *desc, const void *kv, const void *
                           void *codec_workspace, uint64_t codec_workspace_bytes,
                           void *after_scores, void *stream);
 
+/* ------------------------------------------------------------------ the resident cache in use */
+
+/* What a served context does between Load and Reclaim (Sec. 3.1: inference runs on the resident chunks): a new token
+ * attends to the context's cached tokens, and a context may be shrunk to the tokens that attention weighs most.  Both
+ * calls work on a pool of chunk slots (`desc` as for the codec calls, n_tokens = slots * chunk_len; group_size and
+ * quant_mode are not used) and on a batch of sequences, each with a row of a chunk table:
+ *   chunk_table  device int32 [n_seqs][table_stride]: slot of chunk i of sequence b.  Only entries of chunks that hold
+ *                one of the sequence's lens[b] tokens are read; the others may hold anything
+ *   lens         device int32 [n_seqs]: tokens of sequence b in the cache, 0 .. max_len (0: an empty row of the batch)
+ *   max_len      1 .. table_stride * chunk_len: an upper bound of lens known on the host
+ * Token t of sequence b lies in row chunk_table[b][t / chunk_len] * chunk_len + t % chunk_len of every slab.  Values in
+ * rows that no token lies in (the rest of a last chunk) have no influence, infinities and NaN included.
+ * Tables and lengths are read by the device, so a call can be captured into a graph and replayed after they have changed.
+ * head_dim is at most 256 here (LLMS_ERR_UNSUPPORTED otherwise), n_seqs at most 4096. */
+typedef enum llms_dtype { LLMS_F16 = 0, LLMS_BF16 = 1 } llms_dtype;
+
+/* Attention of one new token per sequence, one layer:  for KV head h and each of the n_q_heads / n_kv_heads query
+ * heads g that read it (query head h * (n_q_heads / n_kv_heads) + i), over t in [max(0, lens[b] - window), lens[b])
+ *     s_t = scale * <q[b][g], K_t>;   lse = log sum_t exp(s_t);   out[b][g] = sum_t exp(s_t - lse) * V_t
+ * and, where mass_out is given, for every t < lens[b] (weight 0 outside the window)
+ *     mass_out[b][h][t] = mass_in[b][h][t] + sum over those query heads of exp(s_t - lse).
+ * A sequence without tokens, or with nothing but weights of 0 (all s_t = -inf), gives out = 0 and lse = -inf.  Sums are kept
+ * in binary32 (the products of the weights with V take the weights as a pair of 16-bit values, 16 or more bits together).
+ *   dtype     type of kv, q, k_new, v_new and out (llms_dtype; the codec calls take LLMS_F16 only)
+ *   kv        device, the pool, 16-byte aligned
+ *   q         device [n_seqs] rows of n_q_heads * head_dim elements, q_stride elements apart; 16-byte aligned, q_stride a
+ *             multiple of 8
+ *   k_new, v_new  device [n_seqs] rows of n_kv_heads * head_dim elements, new_stride elements apart (aligned like q), or
+ *             both NULL.  If given, they are K and V of the newest token, t = lens[b] - 1: the call stores them in the
+ *             pool and uses them.  A slot that holds a newest token must then not be listed by another sequence
+ *   window    0: every cached token is seen, else the last `window` ones
+ *   out       device [n_seqs][n_q_heads][head_dim], 16-byte aligned
+ *   lse       device fp32 [n_seqs][n_q_heads], or NULL
+ *   mass_in, mass_out  device fp32 [n_seqs][n_kv_heads][mass_stride], mass_stride >= max_len.  Both NULL: no weights.
+ *             mass_in NULL: taken as zeros.  They may be the same array (accumulation in place) but not overlap otherwise.
+ *             Entries of mass_out from lens[b] on are left as they were
+ *   workspace device, 256-byte aligned, llms_decode_workspace_bytes(desc, n_seqs, max_len, mass_out != NULL); may be
+ *             reused by the next call on the same stream
+ * A sequence whose length is outside 0 .. max_len, or that lists a slot outside the pool, gets NaN in out and lse; nothing
+ * outside the pool is read or written. */
+int llms_decode_workspace_bytes(const llms_kv_desc *desc, int n_seqs, int max_len, int with_mass, uint64_t *nbytes);
+int llms_decode_attention(const llms_kv_desc *desc, int dtype, int layer, void *kv, const void *q, int64_t q_stride,
+                          const void *k_new, const void *v_new, int64_t new_stride, const int32_t *chunk_table,
+                          int table_stride, const int32_t *lens, int n_seqs, int max_len, int window, float scale,
+                          void *out, float *lse, const float *mass_in, float *mass_out, int64_t mass_stride,
+                          void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Token eviction by accumulated attention weight, all layers: sequence b keeps m = min(budget, lens[b]) tokens per layer
+ * and KV head - the last min(recent, m) ones, and of the others those with the largest mass (equal masses: the lower
+ * index; NaN and -inf count as the lowest value).  The kept tokens' K and V rows move, in the order of their positions,
+ * to positions 0 .. m-1, their masses with them.  Elements of 2 bytes are moved whatever their type.
+ *   mass      device fp32 [n_layers][n_seqs][n_kv_heads][mass_stride], as llms_decode_attention accumulates it
+ *   budget    >= 1;  recent  0 .. budget
+ *   dst_table device int32 [n_seqs][dst_stride], dst_stride * chunk_len >= min(budget, max_len): where positions 0 .. m-1
+ *             go.  Every slot listed there (for those positions) must be one that this call does not read, and listed once.
+ *             NULL: the rows stay in the sequence's own chunks (in place; then a slot must not be listed by two sequences)
+ *   mass_out  like mass, may be the same array but not overlap it otherwise: masses of positions 0 .. m-1, then zeros up to
+ *             lens[b]; entries from lens[b] on are left as they were
+ *   kept      device int32 [n_layers][n_seqs][n_kv_heads][budget]: the kept positions, ascending, then -1
+ *   new_lens  device int32 [n_seqs], not the same array as lens: m (-1 where lens[b] is outside 0 .. max_len: such a
+ *             sequence is left as it is and its kept is all -1)
+ * A row whose slot, or whose new slot, lies outside the pool is neither read nor written. */
+int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float *mass, int64_t mass_stride,
+                      const int32_t *chunk_table, int table_stride, const int32_t *lens, int n_seqs, int max_len,
+                      int budget, int recent, const int32_t *dst_table, int dst_stride, float *mass_out,
+                      int32_t *kept, int32_t *new_lens, void *stream);
+
 /* ------------------------------------------------------------------ swap copies */
 
 /* Copy n records between a device swap buffer and a pinned host arena on `side_stream`

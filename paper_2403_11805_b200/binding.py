@@ -68,6 +68,14 @@ _SIGNATURES = {
     "llms_compress_context": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p, C.c_uint64,
                                         C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]),
+    "llms_decode_workspace_bytes": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p]),
+    "llms_decode_attention": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                        C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_float,
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_uint64,
+                                        C.c_void_p]),
+    "llms_evict_tokens": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int,
+                                    C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
+                                    C.c_void_p]),
     "llms_lctru_order": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p]),
     "llms_swap_out": (C.c_int, [C.c_void_p, C.c_uint64, C.c_void_p, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p,
                                 C.c_void_p, C.c_void_p, C.c_void_p]),
@@ -354,6 +362,133 @@ def compress_context(desc, kv, q_win, W, frac, levels, scores_dev, scores_host, 
         C.addressof(desc), _ptr(kv), _ptr(q_win), int(W), _ptr(frac), _ptr(levels), _ptr(scores_dev), _ptr(scores_host),
         _ptr(bits_out), _ptr(out_buf), _nbytes(out_buf), _ptr(meta), _ptr(tolerance_workspace), _nbytes(tolerance_workspace),
         _ptr(codec_workspace), _nbytes(codec_workspace), _event(after_scores), _stream(stream)), "llms_compress_context")
+
+
+# ----------------------------------------------------------------------------- the resident cache in use
+
+DTYPE_F16, DTYPE_BF16 = 0, 1
+
+
+def _refuse(what):
+    raise LlmsError(ERR_INVALID_ARG, what)
+
+
+def _dtype_of(x):
+    name = str(x.dtype)
+    if name == "torch.float16":
+        return DTYPE_F16
+    if name == "torch.bfloat16":
+        return DTYPE_BF16
+    raise LlmsError(ERR_UNSUPPORTED, f"a cache of {name} (float16 and bfloat16 are taken)")
+
+
+def _on_device(what, *tensors):
+    """The library works on the current device: a tensor of another one, or of the host, is refused."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            _refuse(f"{what}: a tensor on {t.device} in a call on cuda:{here}")
+
+
+def _rows_of(x, n, width, dtype, what):
+    """(address, elements from one sequence to the next) of a [n, heads, head_dim] tensor: a sequence's heads lie side by side,
+    the sequences any number of elements apart (q, k and v may be views of one projection's output)."""
+    if x.dim() != 3 or x.shape[0] != n or x.shape[1] * x.shape[2] != width or x.dtype != dtype:
+        _refuse(f"{what}: {tuple(x.shape)} of {x.dtype}, [{n}, heads, head_dim] with {width} elements of {dtype} each wanted")
+    st = x.stride()
+    if (x.shape[2] > 1 and st[2] != 1) or (x.shape[1] > 1 and st[1] != x.shape[2]):
+        _refuse(f"{what}: a sequence's heads must lie side by side")
+    return x.data_ptr(), (st[0] if n > 1 else width)
+
+
+def _whole(x, shape, name, what):
+    """Address of a contiguous tensor that must have this shape and type."""
+    if tuple(x.shape) != shape or not str(x.dtype).endswith(name) or not x.is_contiguous():
+        _refuse(f"{what}: {tuple(x.shape)} of {x.dtype}, a contiguous {shape} of {name} wanted")
+    return x.data_ptr()
+
+
+def _batch(chunk_table, lens, what):
+    """(address, row stride) of an int32 chunk table [n_seqs, chunks], address of the lengths."""
+    n = lens.shape[0]
+    if chunk_table.dim() != 2 or chunk_table.shape[0] != n or not str(chunk_table.dtype).endswith(".int32") or not (
+            chunk_table.shape[1] == 1 or chunk_table.stride(1) == 1):
+        _refuse(f"{what}: chunk_table must be int32 [n_seqs, chunks] with its rows' entries side by side")
+    return chunk_table.data_ptr(), (chunk_table.stride(0) if n > 1 else chunk_table.shape[1]), _whole(lens, (n,), ".int32", f"{what}: lens")
+
+
+def decode_workspace_bytes(desc, n_seqs, max_len, with_mass=False):
+    nb = C.c_uint64()
+    _check(lib().llms_decode_workspace_bytes(C.addressof(desc), int(n_seqs), int(max_len), int(with_mass), C.addressof(nb)),
+           "llms_decode_workspace_bytes")
+    return nb.value
+
+
+def decode_attention(desc, layer, kv, q, chunk_table, lens, max_len, out, workspace, k_new=None, v_new=None, window=0, scale=None,
+                     lse=None, mass_in=None, mass_out=None, stream=None):
+    """llms_decode_attention: one new token per sequence attends to its cached tokens, in one layer of the pool.
+    kv: the pool (fp16 or bf16, device); q, out: [n_seqs, n_q_heads, head_dim]; k_new, v_new: [n_seqs, n_kv_heads, head_dim],
+    stored at position lens - 1; chunk_table: int32 [n_seqs, chunks]; lens: int32 [n_seqs]; scale: 1/sqrt(head_dim) if None;
+    lse: fp32 [n_seqs, n_q_heads]; mass_in, mass_out: fp32 [n_seqs, n_kv_heads, >= max_len]."""
+    what = "llms_decode_attention"
+    n, d = lens.shape[0], desc.head_dim
+    _on_device(what, kv, q, chunk_table, lens, out, workspace, k_new, v_new, lse, mass_in, mass_out)
+    dtype = _dtype_of(kv)
+    q_ptr, q_stride = _rows_of(q, n, desc.n_q_heads * d, kv.dtype, f"{what}: q")
+    k_ptr = v_ptr = None
+    new_stride = 0
+    if k_new is not None or v_new is not None:
+        if k_new is None or v_new is None:
+            _refuse(f"{what}: k_new and v_new come together")
+        k_ptr, new_stride = _rows_of(k_new, n, desc.n_kv_heads * d, kv.dtype, f"{what}: k_new")
+        v_ptr, v_stride = _rows_of(v_new, n, desc.n_kv_heads * d, kv.dtype, f"{what}: v_new")
+        if v_stride != new_stride:
+            _refuse(f"{what}: k_new and v_new must have the same stride")
+    table_ptr, table_stride, lens_ptr = _batch(chunk_table, lens, what)
+    if table_stride < chunk_table.shape[1] or chunk_table.shape[1] * desc.chunk_len < max_len:
+        _refuse(f"{what}: max_len {max_len} is more than {chunk_table.shape[1]} chunks of a table row hold")
+    if out.dtype != kv.dtype or out.numel() != n * desc.n_q_heads * d or not out.is_contiguous():
+        _refuse(f"{what}: out must be a contiguous [{n}, {desc.n_q_heads}, {d}] of {kv.dtype}")
+    in_ptr = out_mass = None
+    mass_stride = 0
+    if mass_out is not None:
+        mass_stride = mass_out.shape[-1]
+        out_mass = _whole(mass_out, (n, desc.n_kv_heads, mass_stride), ".float32", f"{what}: mass_out")
+    if mass_in is not None:
+        in_ptr = _whole(mass_in, (n, desc.n_kv_heads, mass_stride), ".float32", f"{what}: mass_in")
+    _check(lib().llms_decode_attention(
+        C.addressof(desc), dtype, layer, kv.data_ptr(), q_ptr, q_stride, k_ptr, v_ptr, new_stride, table_ptr, table_stride, lens_ptr,
+        n, max_len, window, d ** -0.5 if scale is None else scale, out.data_ptr(),
+        None if lse is None else _whole(lse, (n, desc.n_q_heads), ".float32", f"{what}: lse"), in_ptr, out_mass, mass_stride,
+        workspace.data_ptr(), _nbytes(workspace), _stream(stream)), what)
+
+
+def evict_tokens(desc, kv, mass, chunk_table, lens, max_len, budget, recent, kept, new_lens, mass_out=None, dst_table=None,
+                 stream=None):
+    """llms_evict_tokens: per layer and KV head the `budget` heaviest tokens stay (the last `recent` in any case).
+    mass, mass_out: fp32 [n_layers, n_seqs, n_kv_heads, >= max_len] (mass_out None: in place); kept: int32 [n_layers, n_seqs,
+    n_kv_heads, budget]; new_lens: int32 [n_seqs]; dst_table: int32 [n_seqs, chunks] or None (rows stay in their chunks)."""
+    what = "llms_evict_tokens"
+    n = lens.shape[0]
+    _on_device(what, kv, mass, chunk_table, lens, kept, new_lens, mass_out, dst_table)
+    if kv.element_size() != 2:
+        _refuse(f"{what}: elements of 2 bytes are moved, not {kv.dtype}")
+    shape = (desc.n_layers, n, desc.n_kv_heads, mass.shape[-1])
+    table_ptr, table_stride, lens_ptr = _batch(chunk_table, lens, what)
+    if table_stride < chunk_table.shape[1] or chunk_table.shape[1] * desc.chunk_len < max_len:
+        _refuse(f"{what}: max_len {max_len} is more than {chunk_table.shape[1]} chunks of a table row hold")
+    dst_ptr, dst_stride = None, 0
+    if dst_table is not None:
+        dst_ptr, dst_stride, _ = _batch(dst_table, lens, f"{what}: dst_table")
+        if dst_stride < dst_table.shape[1] or dst_table.shape[1] * desc.chunk_len < min(budget, max_len):
+            _refuse(f"{what}: {dst_table.shape[1]} chunks of a dst_table row do not hold {min(budget, max_len)} tokens")
+    mass_ptr = _whole(mass, shape, ".float32", f"{what}: mass")
+    _check(lib().llms_evict_tokens(
+        C.addressof(desc), kv.data_ptr(), mass_ptr, shape[3], table_ptr, table_stride, lens_ptr, n, max_len, budget, recent,
+        dst_ptr, dst_stride, mass_ptr if mass_out is None else _whole(mass_out, shape, ".float32", f"{what}: mass_out"),
+        _whole(kept, shape[:3] + (budget,), ".int32", f"{what}: kept"), _whole(new_lens, (n,), ".int32", f"{what}: new_lens"),
+        _stream(stream)), what)
 
 
 # ----------------------------------------------------------------------------- swap

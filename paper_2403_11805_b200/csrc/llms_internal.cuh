@@ -61,6 +61,8 @@ inline uint64_t groups_per_chunk(const llms_kv_desc &d) { return (uint64_t)slabs
 int check_desc(const llms_kv_desc *d);
 // Shape + alignment checks for the codec kernels (vector loads need 16-byte aligned slabs).
 int check_desc_codec(const llms_kv_desc *d);
+// Shape checks of the calls that use a paged cache: a pool the codec could take, with head_dim up to 256, and a batch.
+int check_paged(const llms_kv_desc *d, int n_seqs, int max_len);
 inline int check_bits(int b) { return (b == 1 || b == 2 || b == 4 || b == 8) ? LLMS_OK : LLMS_ERR_BAD_BITS; }
 
 // Number of SMs of the current device (cached per device).
