@@ -33,7 +33,7 @@
 // (not kept); with two tiles per MMA (this kernel) the score stage of the 32K shape went from 384 to 357 us.
 #pragma once
 
-#include <cuda.h>
+#include "tma.cuh"
 
 namespace llms {
 
@@ -43,7 +43,6 @@ constexpr int kTcAcc = 4;                            // tile-wide halves of the 
 constexpr int kTcEpiWarps = 4 * kTcAcc;              // per accumulator one warp for each quarter of the 128 lanes
 constexpr int kTcProducerWarp = kTcEpiWarps, kTcMmaWarp = kTcEpiWarps + 1;
 constexpr int kTcThreads = (kTcEpiWarps + 2) * 32;
-constexpr uint32_t kTcSpinLimit = 1u << 22;          // polls (with a pause in between) before a wait is given up
 constexpr uint32_t kTcGaveUp = 0x7E57DEADu;          // value of the status word after a wait was given up
 constexpr int kTcBlockBytes = kTcTile * 128;         // one 64-channel block of the 128-row A operand: 128 rows x 128 bytes
 constexpr int kTcWideBlockBytes = kTcWide * 128;     // one 64-channel block of the 256-row B operand (two tiles of K)
@@ -55,48 +54,6 @@ struct TcBarriers {
     uint32_t tmem_base;
     uint32_t gave_up;
 };
-
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(unsigned long long *bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(smem_u32(bar)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(unsigned long long *bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(unsigned long long *bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
-// Wait for the phase of the given parity to complete; false when the wait was given up.
-__device__ __forceinline__ bool mbar_wait(unsigned long long *bar, uint32_t parity, volatile uint32_t *gave_up)
-{
-    const uint32_t addr = smem_u32(bar);
-    for (uint32_t i = 0; i < kTcSpinLimit; ++i) {
-        uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-                     : "=r"(done) : "r"(addr), "r"(parity) : "memory");
-        if (done) return true;
-        if (*gave_up) return false;                   // another role has given up: no point in waiting on
-        if (i > 32) __nanosleep(64);
-    }
-    *gave_up = 1;
-    return false;
-}
-
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int c0, int c1, unsigned long long *bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 :: "r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1) : "memory");
-}
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3,
-                                            unsigned long long *bar)
-{
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-                 :: "r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
-}
 
 // Shared-memory operand descriptor: rows of 128 bytes (64 fp16 channels, the contraction dimension contiguous), 128-byte
 // swizzle, groups of eight rows 1024 bytes apart.  Fields: address / 16 in bits 0-13, leading offset (1, unused with a
