@@ -286,7 +286,7 @@ int llms_compress_context(const llms_kv_desc *desc, const void *kv, const void *
  * Token t of sequence b lies in row chunk_table[b][t / chunk_len] * chunk_len + t % chunk_len of every slab.  Values in
  * rows that no token lies in (the rest of a last chunk) have no influence, infinities and NaN included.
  * Tables and lengths are read by the device, so a call can be captured into a graph and replayed after they have changed.
- * head_dim is at most 256 here (LLMS_ERR_UNSUPPORTED otherwise), n_seqs at most 4096. */
+ * head_dim is at most 256 here, n_seqs at most 4096, n_q_heads at most 65535 (LLMS_ERR_UNSUPPORTED otherwise). */
 typedef enum llms_dtype { LLMS_F16 = 0, LLMS_BF16 = 1 } llms_dtype;
 
 /* Attention of one new token per sequence, one layer:  for KV head h and each of the n_q_heads / n_kv_heads query

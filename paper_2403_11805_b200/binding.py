@@ -367,55 +367,48 @@ def compress_context(desc, kv, q_win, W, frac, levels, scores_dev, scores_host, 
 # ----------------------------------------------------------------------------- the resident cache in use
 
 DTYPE_F16, DTYPE_BF16 = 0, 1
+# These calls come once per layer and token, so their argument checks are written as one condition each; what is wrong is
+# worked out only after it has failed.
+_torch = None
 
 
-def _refuse(what):
-    raise LlmsError(ERR_INVALID_ARG, what)
+def _current(stream):
+    """(current device, address of the stream: the current one if None)"""
+    global _torch
+    if _torch is None:
+        import torch
+        torch.cuda.init()
+        _torch = torch
+    device = _torch._C._cuda_getDevice()
+    if stream is None:
+        return device, _torch._C._cuda_getCurrentRawStream(device)
+    return device, stream if isinstance(stream, int) else stream.cuda_stream
 
 
-def _dtype_of(x):
-    name = str(x.dtype)
-    if name == "torch.float16":
-        return DTYPE_F16
-    if name == "torch.bfloat16":
-        return DTYPE_BF16
-    raise LlmsError(ERR_UNSUPPORTED, f"a cache of {name} (float16 and bfloat16 are taken)")
+def _is_rows(x, n, heads, d, dtype, device):
+    """[n, heads, d] with a sequence's heads side by side; the sequences may be any number of elements apart."""
+    if x.shape != (n, heads, d) or x.dtype is not dtype or x.get_device() != device:
+        return False
+    _, head, channel = x.stride()
+    return channel == 1 and (head == d or heads == 1)
 
 
-def _on_device(what, *tensors):
-    """The library works on the current device: a tensor of another one, or of the host, is refused."""
-    import torch
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            _refuse(f"{what}: a tensor on {t.device} in a call on cuda:{here}")
+def _is_whole(x, shape, dtype, device):
+    return x.shape == shape and x.dtype is dtype and x.get_device() == device and x.is_contiguous()
 
 
-def _rows_of(x, n, width, dtype, what):
-    """(address, elements from one sequence to the next) of a [n, heads, head_dim] tensor: a sequence's heads lie side by side,
-    the sequences any number of elements apart (q, k and v may be views of one projection's output)."""
-    if x.dim() != 3 or x.shape[0] != n or x.shape[1] * x.shape[2] != width or x.dtype != dtype:
-        _refuse(f"{what}: {tuple(x.shape)} of {x.dtype}, [{n}, heads, head_dim] with {width} elements of {dtype} each wanted")
-    st = x.stride()
-    if (x.shape[2] > 1 and st[2] != 1) or (x.shape[1] > 1 and st[1] != x.shape[2]):
-        _refuse(f"{what}: a sequence's heads must lie side by side")
-    return x.data_ptr(), (st[0] if n > 1 else width)
+def _is_batch(table, lens, device):
+    i32 = _torch.int32
+    return (table.dtype is i32 and lens.dtype is i32 and table.get_device() == device and lens.get_device() == device
+            and table.dim() == 2 and lens.dim() == 1 and table.shape[0] == lens.shape[0] and lens.is_contiguous()
+            and (table.stride(1) == 1 or table.shape[1] == 1))
 
 
-def _whole(x, shape, name, what):
-    """Address of a contiguous tensor that must have this shape and type."""
-    if tuple(x.shape) != shape or not str(x.dtype).endswith(name) or not x.is_contiguous():
-        _refuse(f"{what}: {tuple(x.shape)} of {x.dtype}, a contiguous {shape} of {name} wanted")
-    return x.data_ptr()
-
-
-def _batch(chunk_table, lens, what):
-    """(address, row stride) of an int32 chunk table [n_seqs, chunks], address of the lengths."""
-    n = lens.shape[0]
-    if chunk_table.dim() != 2 or chunk_table.shape[0] != n or not str(chunk_table.dtype).endswith(".int32") or not (
-            chunk_table.shape[1] == 1 or chunk_table.stride(1) == 1):
-        _refuse(f"{what}: chunk_table must be int32 [n_seqs, chunks] with its rows' entries side by side")
-    return chunk_table.data_ptr(), (chunk_table.stride(0) if n > 1 else chunk_table.shape[1]), _whole(lens, (n,), ".int32", f"{what}: lens")
+def _refuse(what, device, wanted, **tensors):
+    """Arguments that do not fit: names what was given."""
+    given = ", ".join(f"{k} " + ("none" if x is None else f"{tuple(x.shape)} {x.dtype} strides {tuple(x.stride())} on {x.device}")
+                      for k, x in tensors.items())
+    raise LlmsError(ERR_INVALID_ARG, f"{what} on cuda:{device}: {wanted}; given: {given}")
 
 
 def decode_workspace_bytes(desc, n_seqs, max_len, with_mass=False):
@@ -430,65 +423,80 @@ def decode_attention(desc, layer, kv, q, chunk_table, lens, max_len, out, worksp
     """llms_decode_attention: one new token per sequence attends to its cached tokens, in one layer of the pool.
     kv: the pool (fp16 or bf16, device); q, out: [n_seqs, n_q_heads, head_dim]; k_new, v_new: [n_seqs, n_kv_heads, head_dim],
     stored at position lens - 1; chunk_table: int32 [n_seqs, chunks]; lens: int32 [n_seqs]; scale: 1/sqrt(head_dim) if None;
-    lse: fp32 [n_seqs, n_q_heads]; mass_in, mass_out: fp32 [n_seqs, n_kv_heads, >= max_len]."""
+    lse: fp32 [n_seqs, n_q_heads]; mass_in, mass_out: fp32 [n_seqs, n_kv_heads, >= max_len].  q, k_new and v_new may be views
+    of one projection's output.  All tensors on the current device."""
     what = "llms_decode_attention"
-    n, d = lens.shape[0], desc.head_dim
-    _on_device(what, kv, q, chunk_table, lens, out, workspace, k_new, v_new, lse, mass_in, mass_out)
-    dtype = _dtype_of(kv)
-    q_ptr, q_stride = _rows_of(q, n, desc.n_q_heads * d, kv.dtype, f"{what}: q")
-    k_ptr = v_ptr = None
-    new_stride = 0
+    device, stream = _current(stream)
+    n, d, hq, hk, dtype = lens.shape[0], desc.head_dim, desc.n_q_heads, desc.n_kv_heads, kv.dtype
+    f32 = _torch.float32
+    if dtype is _torch.float16:
+        code = DTYPE_F16
+    elif dtype is _torch.bfloat16:
+        code = DTYPE_BF16
+    else:
+        raise LlmsError(ERR_UNSUPPORTED, f"{what}: a cache of {dtype} (float16 and bfloat16 are taken)")
+    if not (_is_batch(chunk_table, lens, device) and kv.get_device() == device and workspace.get_device() == device
+            and _is_rows(q, n, hq, d, dtype, device) and _is_whole(out, (n, hq, d), dtype, device)
+            and (lse is None or _is_whole(lse, (n, hq), f32, device))):
+        _refuse(what, device, f"kv on this device, chunk_table int32 [{n}, chunks], lens int32 [{n}], q and out [{n}, {hq}, {d}] of kv's type, "
+                f"lse float32 [{n}, {hq}]", kv=kv, chunk_table=chunk_table, lens=lens, q=q, out=out, lse=lse, workspace=workspace)
+    chunks = chunk_table.shape[1]
+    if chunks * desc.chunk_len < max_len:
+        _refuse(what, device, f"max_len {max_len} is more than a table row's chunks of {desc.chunk_len} hold", chunk_table=chunk_table)
+    k_ptr = v_ptr = in_ptr = out_ptr = None
+    new_stride = mass_stride = 0
     if k_new is not None or v_new is not None:
-        if k_new is None or v_new is None:
-            _refuse(f"{what}: k_new and v_new come together")
-        k_ptr, new_stride = _rows_of(k_new, n, desc.n_kv_heads * d, kv.dtype, f"{what}: k_new")
-        v_ptr, v_stride = _rows_of(v_new, n, desc.n_kv_heads * d, kv.dtype, f"{what}: v_new")
-        if v_stride != new_stride:
-            _refuse(f"{what}: k_new and v_new must have the same stride")
-    table_ptr, table_stride, lens_ptr = _batch(chunk_table, lens, what)
-    if table_stride < chunk_table.shape[1] or chunk_table.shape[1] * desc.chunk_len < max_len:
-        _refuse(f"{what}: max_len {max_len} is more than {chunk_table.shape[1]} chunks of a table row hold")
-    if out.dtype != kv.dtype or out.numel() != n * desc.n_q_heads * d or not out.is_contiguous():
-        _refuse(f"{what}: out must be a contiguous [{n}, {desc.n_q_heads}, {d}] of {kv.dtype}")
-    in_ptr = out_mass = None
-    mass_stride = 0
-    if mass_out is not None:
-        mass_stride = mass_out.shape[-1]
-        out_mass = _whole(mass_out, (n, desc.n_kv_heads, mass_stride), ".float32", f"{what}: mass_out")
-    if mass_in is not None:
-        in_ptr = _whole(mass_in, (n, desc.n_kv_heads, mass_stride), ".float32", f"{what}: mass_in")
-    _check(lib().llms_decode_attention(
-        C.addressof(desc), dtype, layer, kv.data_ptr(), q_ptr, q_stride, k_ptr, v_ptr, new_stride, table_ptr, table_stride, lens_ptr,
-        n, max_len, window, d ** -0.5 if scale is None else scale, out.data_ptr(),
-        None if lse is None else _whole(lse, (n, desc.n_q_heads), ".float32", f"{what}: lse"), in_ptr, out_mass, mass_stride,
-        workspace.data_ptr(), _nbytes(workspace), _stream(stream)), what)
+        if not (k_new is not None and v_new is not None and _is_rows(k_new, n, hk, d, dtype, device)
+                and _is_rows(v_new, n, hk, d, dtype, device) and (n == 1 or k_new.stride(0) == v_new.stride(0))):
+            _refuse(what, device, f"k_new and v_new together, [{n}, {hk}, {d}] of kv's type with the same strides", k_new=k_new, v_new=v_new)
+        k_ptr, v_ptr, new_stride = k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0) if n > 1 else hk * d
+    if mass_out is not None or mass_in is not None:
+        mass_stride = 0 if mass_out is None else mass_out.shape[-1]
+        if not (mass_out is not None and _is_whole(mass_out, (n, hk, mass_stride), f32, device)
+                and (mass_in is None or _is_whole(mass_in, (n, hk, mass_stride), f32, device))):
+            _refuse(what, device, f"mass_out float32 [{n}, {hk}, >= {max_len}], mass_in none or like it", mass_in=mass_in, mass_out=mass_out)
+        out_ptr, in_ptr = mass_out.data_ptr(), None if mass_in is None else mass_in.data_ptr()
+    rc = (_lib or lib()).llms_decode_attention(
+        C.addressof(desc), code, layer, kv.data_ptr(), q.data_ptr(), q.stride(0) if n > 1 else hq * d, k_ptr, v_ptr, new_stride,
+        chunk_table.data_ptr(), chunk_table.stride(0) if n > 1 else chunks, lens.data_ptr(), n, max_len, window,
+        d ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(), in_ptr, out_ptr, mass_stride,
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+    if rc < 0:
+        raise LlmsError(rc, what)
 
 
 def evict_tokens(desc, kv, mass, chunk_table, lens, max_len, budget, recent, kept, new_lens, mass_out=None, dst_table=None,
                  stream=None):
     """llms_evict_tokens: per layer and KV head the `budget` heaviest tokens stay (the last `recent` in any case).
     mass, mass_out: fp32 [n_layers, n_seqs, n_kv_heads, >= max_len] (mass_out None: in place); kept: int32 [n_layers, n_seqs,
-    n_kv_heads, budget]; new_lens: int32 [n_seqs]; dst_table: int32 [n_seqs, chunks] or None (rows stay in their chunks)."""
+    n_kv_heads, budget]; new_lens: int32 [n_seqs]; dst_table: int32 [n_seqs, chunks] or None (rows stay in their chunks).
+    All tensors on the current device."""
     what = "llms_evict_tokens"
-    n = lens.shape[0]
-    _on_device(what, kv, mass, chunk_table, lens, kept, new_lens, mass_out, dst_table)
-    if kv.element_size() != 2:
-        _refuse(f"{what}: elements of 2 bytes are moved, not {kv.dtype}")
-    shape = (desc.n_layers, n, desc.n_kv_heads, mass.shape[-1])
-    table_ptr, table_stride, lens_ptr = _batch(chunk_table, lens, what)
-    if table_stride < chunk_table.shape[1] or chunk_table.shape[1] * desc.chunk_len < max_len:
-        _refuse(f"{what}: max_len {max_len} is more than {chunk_table.shape[1]} chunks of a table row hold")
-    dst_ptr, dst_stride = None, 0
+    device, stream = _current(stream)
+    n, hk, layers = lens.shape[0], desc.n_kv_heads, desc.n_layers
+    f32, i32 = _torch.float32, _torch.int32
+    tokens = mass.shape[-1]
+    shape = (layers, n, hk, tokens)
+    if not (_is_batch(chunk_table, lens, device) and kv.get_device() == device and kv.element_size() == 2
+            and _is_whole(mass, shape, f32, device) and (mass_out is None or _is_whole(mass_out, shape, f32, device))
+            and _is_whole(kept, (layers, n, hk, budget), i32, device) and _is_whole(new_lens, (n,), i32, device)):
+        _refuse(what, device, f"kv of 2-byte elements on this device, chunk_table int32 [{n}, chunks], lens and new_lens int32 [{n}], mass and "
+                f"mass_out float32 [{layers}, {n}, {hk}, >= {max_len}], kept int32 [{layers}, {n}, {hk}, {budget}]", kv=kv,
+                chunk_table=chunk_table, lens=lens, mass=mass, mass_out=mass_out, kept=kept, new_lens=new_lens)
+    chunks, dst_ptr, dst_stride = chunk_table.shape[1], None, 0
+    if chunks * desc.chunk_len < max_len:
+        _refuse(what, device, f"max_len {max_len} is more than a table row's chunks of {desc.chunk_len} hold", chunk_table=chunk_table)
     if dst_table is not None:
-        dst_ptr, dst_stride, _ = _batch(dst_table, lens, f"{what}: dst_table")
-        if dst_stride < dst_table.shape[1] or dst_table.shape[1] * desc.chunk_len < min(budget, max_len):
-            _refuse(f"{what}: {dst_table.shape[1]} chunks of a dst_table row do not hold {min(budget, max_len)} tokens")
-    mass_ptr = _whole(mass, shape, ".float32", f"{what}: mass")
-    _check(lib().llms_evict_tokens(
-        C.addressof(desc), kv.data_ptr(), mass_ptr, shape[3], table_ptr, table_stride, lens_ptr, n, max_len, budget, recent,
-        dst_ptr, dst_stride, mass_ptr if mass_out is None else _whole(mass_out, shape, ".float32", f"{what}: mass_out"),
-        _whole(kept, shape[:3] + (budget,), ".int32", f"{what}: kept"), _whole(new_lens, (n,), ".int32", f"{what}: new_lens"),
-        _stream(stream)), what)
+        if not (_is_batch(dst_table, lens, device) and dst_table.shape[1] * desc.chunk_len >= min(budget, max_len)):
+            _refuse(what, device, f"dst_table int32 [{n}, chunks] with room for {min(budget, max_len)} tokens", dst_table=dst_table)
+        dst_ptr, dst_stride = dst_table.data_ptr(), dst_table.stride(0) if n > 1 else dst_table.shape[1]
+    mass_ptr = mass.data_ptr()
+    rc = (_lib or lib()).llms_evict_tokens(
+        C.addressof(desc), kv.data_ptr(), mass_ptr, tokens, chunk_table.data_ptr(), chunk_table.stride(0) if n > 1 else chunks, lens.data_ptr(),
+        n, max_len, budget, recent, dst_ptr, dst_stride, mass_ptr if mass_out is None else mass_out.data_ptr(), kept.data_ptr(),
+        new_lens.data_ptr(), stream)
+    if rc < 0:
+        raise LlmsError(rc, what)
 
 
 # ----------------------------------------------------------------------------- swap

@@ -69,7 +69,7 @@ int check_paged(const llms_kv_desc *d, int n_seqs, int max_len)
     if (rc) return rc;
     if (d->head_dim % 16 || (d->stride_l | d->stride_s | d->stride_h) % 8) return LLMS_ERR_MISALIGNED;
     if (n_seqs < 0 || max_len < 1) return LLMS_ERR_INVALID_ARG;
-    if (d->head_dim > 256 || n_seqs > 4096 || d->n_kv_heads > 65535) return LLMS_ERR_UNSUPPORTED;
+    if (d->head_dim > 256 || n_seqs > 4096 || d->n_q_heads > 65535) return LLMS_ERR_UNSUPPORTED;
     // everything a batch can hold is counted in 32 bits: 16-token tiles of all KV heads and query heads of all sequences
     if ((uint64_t)n_seqs * d->n_q_heads * ((uint64_t)max_len / 16 + 1) > 0x7fffffffu) return LLMS_ERR_UNSUPPORTED;
     return LLMS_OK;

@@ -9,14 +9,15 @@
 // with eight query rows (m16n8k16, tokens or channels on the 16 side) keep that arithmetic far below the memory time;
 // a tcgen05 MMA has at least 64 rows and would multiply mostly padding.
 //
-// Split.  The work is the sequence of all 16-token tiles of all (sequence, KV head) items of the batch.  It is cut into equal
-// runs, one per CTA, and each into equal runs per warp, whatever the sequences' lengths: the lengths are known on the
-// device only, and equal runs balance ragged batches and long single contexts alike.  A warp feeds itself: its lane 0
-// (with chunks shorter than a tile, a lane per piece of the tile) asks for tiles a ring of stages ahead by TMA, 64
-// channels x 16 tokens at a time, 128-byte swizzled; nothing is exchanged between warps until their runs end.  An item that
-// lies in one warp's run is finished by it; the pieces of the others are joined in shared memory at the end of the CTA,
-// and where an item spans CTAs, from the workspace by join_kernel.  All sums have a fixed order: repeated calls agree
-// bit for bit.
+// Split.  The work is the sequence of all 16-token tiles of all items (sequence, KV head, up to 16 query heads of it) of the
+// batch.  It is cut into equal runs, one per warp, whatever the sequences' lengths: the lengths are known on the device only,
+// and equal runs balance ragged batches and long single contexts alike.  A CTA is one warp: nothing is exchanged between
+// warps, so none waits for another, and the hardware hands the next run to whichever SM has room (SMs stream at different
+// speeds; a fixed split over resident warps left the fastest idle for a third of the time).  A warp feeds itself: its lanes
+// look the slots of up to 32 tiles up at once and ask for the tiles by TMA a ring of stages ahead, 128-byte swizzled; with an
+// item's first tile come its query rows.  An item that lies in one run is finished by its warp; the pieces of the others go to
+// the workspace, where finish_kernel joins them; it also turns the logits into the tokens' weights.  All sums have a fixed
+// order: repeated calls agree bit for bit.
 #include <math.h>
 
 #include <algorithm>
@@ -29,14 +30,16 @@
 namespace llms {
 
 constexpr int kTile = 16;                         // tokens per tile: the 16 side of an MMA
-constexpr int kMaxStages = 8;
+constexpr int kQuerySlots = 2;                    // items whose query rows a warp holds: the current one's, the next one's
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// For the product with V a weight 2^(v - m) goes into the MMA as kLift times its value, as a sum of two 16-bit values
-// hi + lo.  hi is cut off a little below the weight, so that lo is never 0: a value of V that is infinite then gives an
-// infinity, not 0 * inf.  The lift (a power of two, taken back exactly at the end) keeps lo a normal fp16 number for
-// weights down to 2^-26 of the largest.  Together the two carry 21 (fp16) or 16 (bf16) bits; one 16-bit value alone would
+// Weights are taken against a reference that follows the running maximum in steps: it moves only when a logit exceeds it by more
+// than kSlack (in units of log2), so most tiles need no maximum over the warp's lanes and no rescaling.
+// For the product with V a weight goes into the MMA as kLift times its value, as a sum of two 16-bit values hi + lo.  hi is cut
+// off a little below the weight, so that lo is never 0: a value of V that is infinite then gives an infinity, not 0 * inf.  The
+// lift (a power of two, taken back exactly at the end) keeps kLift * 2^kSlack in fp16's range and lo a number fp16 can hold for
+// weights down to 2^-18 of the reference.  Together the two carry 21 (fp16) or 16 (bf16) bits; one 16-bit value alone would
 // add an error as large as the rounding of the output itself.
-constexpr float kLift = 16384.0f;
+constexpr float kSlack = 8.0f, kLift = 64.0f;
 
 struct DecodeArgs {
     const uint16_t *q, *k_new, *v_new;
@@ -46,14 +49,19 @@ struct DecodeArgs {
     const float *mass_in;
     float *mass_out;
     float *logits;                                // workspace: v of every (sequence, KV head, token, query head), for the masses
-    float *part;                                  // workspace: two partial results per CTA
-    int32_t *plan;                                // workspace: first tile of every sequence, then the tiles of the batch
+    float *part;                                  // workspace: two partial results per run (rows x (cols + 4): O, m, l): of the item
+                                                  // that began before the run, of the one that goes on behind it
+    int2 *span;                                   // workspace: per item the first and the last run that have tiles of it;
+                                                  // (-1, 0): one run has them all
+    int32_t *open;                                // workspace: per run the item that begins in it and goes on behind it, or -1
     int64_t q_stride, new_stride, stride_h, mass_stride;
     int table_stride, n_seqs, max_len, window, Hkv, Hq, group, d, chunk_len, n_slots;
     int blocks;                                   // blocks of query rows per KV head
     int piece;                                    // tokens per TMA box: the largest power of two up to 16 that divides chunk_len
-    int stages, rows, ctas;                       // ring stages, query rows kept per partial result, CTAs of the main kernel
-    int min_tiles;                                // a CTA takes at least this many tiles
+    int rows, runs;                               // query rows kept per partial result, runs at most (CTAs of the main kernel)
+    int min_tiles;                                // a run has at least this many tiles (but for the last tiles of a small batch)
+    int q_bytes;                                  // of an item's query rows
+    int whole_tile;                               // one TMA copy takes K and V of a tile
     float scale_log2;
 };
 
@@ -71,46 +79,20 @@ __device__ __forceinline__ SeqTiles seq_tiles(const DecodeArgs &a, int len)
     return s;
 }
 
-// CTAs that share the batch's tiles, and who has which
-__device__ __forceinline__ int working_ctas(const DecodeArgs &a, int total) { return min(a.ctas, max(1, total / a.min_tiles)); }
-__device__ __forceinline__ int run_begin(int total, int parts, int i) { return (int)((int64_t)total * i / parts); }
-__device__ __forceinline__ int run_of(int total, int parts, int tile) { return (int)((((int64_t)tile + 1) * parts - 1) / total); }
+// Runs that the batch's tiles are cut into, and which tiles are whose
+__device__ __forceinline__ int working_runs(const DecodeArgs &a, int total) { return min(a.runs, max(1, total / a.min_tiles)); }
+__device__ __forceinline__ int run_begin(int total, int runs, int i) { return (int)((int64_t)total * i / runs); }
+__device__ __forceinline__ int run_of(int total, int runs, int tile) { return (int)((((int64_t)tile + 1) * runs - 1) / total); }
 
-// Where in the batch a tile lies; advanced tile by tile.
-struct Cursor {
-    SeqTiles s;
-    int b, hb, tile;                              // sequence, KV head * blocks + block of query rows, tile of the item
-    __device__ __forceinline__ void start(const DecodeArgs &a, const int32_t *plan, int idx)
-    {
-        int lo = 0, hi = a.n_seqs - 1;            // the last sequence that begins at or before idx
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (plan[mid] <= idx) lo = mid;
-            else hi = mid - 1;
-        }
-        b = lo;
-        s = seq_tiles(a, __ldg(a.lens + b));
-        const int r = idx - plan[b];
-        hb = r / s.n;
-        tile = r - hb * s.n;
-    }
-    __device__ __forceinline__ void next(const DecodeArgs &a)
-    {
-        if (++tile < s.n) return;
-        tile = 0;
-        if (++hb < a.Hkv * a.blocks) return;
-        hb = 0;
-        do {
-            if (++b >= a.n_seqs) return;
-            s = seq_tiles(a, __ldg(a.lens + b));
-        } while (s.n == 0);
-    }
-};
-
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, unsigned long long *bar)
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, int c4, unsigned long long *bar)
 {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-                 :: "r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2) : "memory");
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, unsigned long long *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 :: "r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr)
 {
@@ -169,504 +151,605 @@ __device__ __forceinline__ float2 unpack(uint32_t x)
     return __half22float2(h);
 }
 
-template <int DB> struct DecodeShape {
-    static constexpr int kWarps = DB <= 2 ? 8 : 4;            // warps x stages x tile fill the SM's shared memory
-    static constexpr int kHalf = DB * kTile * 128;            // K (or V) of a tile
-    static constexpr int kStage = 2 * kHalf;
-    static constexpr int kCols = DB * 64;                     // channels, rounded up to whole boxes
-    static constexpr int kPitch = kCols + 4;                  // floats per row of a piece in shared memory
-};
-
-// Shared memory: [1 KiB alignment][warps x stages x tile][first pieces][barriers, piece table][plan].  A warp leaves the piece
-// that its run begins with in its own place of the first-piece area, and the one that its run ends with in its own part of
-// the ring, which has run dry by then.
-// A piece: [rows][kPitch] floats, O in the first kCols columns of a row, then m and l.
-template <int DB>
-__host__ __device__ constexpr size_t piece_floats(int rows) { return (size_t)rows * DecodeShape<DB>::kPitch; }
-
-struct WarpSlots {
-    unsigned long long full[kMaxStages];
-};
-
-template <bool BF, int DB, int NT>
-__global__ void __launch_bounds__(DecodeShape<DB>::kWarps * 32, 1)
-decode_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
-{
-    using S = DecodeShape<DB>;
-    constexpr int W = S::kWarps, KS = DB * 4;                 // k-steps over the channels; also 16-channel tiles of the output
-    extern __shared__ unsigned char smem_raw[];
-    unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    const size_t ring_bytes = (size_t)W * a.stages * S::kStage;
-    float *first_pieces = reinterpret_cast<float *>(ring + ring_bytes);
-    WarpSlots *slots = reinterpret_cast<WarpSlots *>(first_pieces + (size_t)W * piece_floats<DB>(a.rows));
-    int32_t *plan = reinterpret_cast<int32_t *>(slots + W);   // n_seqs + 1
-    __shared__ int piece_item[2 * W], piece_at[2 * W];        // item of every piece left behind (-1: none) and its first tile
-    __shared__ int warp_sum[W];
-    __shared__ uint32_t gave_up;
-
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    unsigned long long *full = slots[warp].full;
-    if (lane == 0) {
-        for (int s = 0; s < a.stages; ++s) mbar_init(&full[s], 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        piece_item[2 * warp] = piece_item[2 * warp + 1] = -1;
-    }
-    if (threadIdx.x == 0) gave_up = 0;
-
-    // tiles before every sequence
-    const int per_seq = a.Hkv * a.blocks;
-    {
-        int base = 0;
-        for (int b0 = 0; b0 < a.n_seqs; b0 += W * 32) {
-            const int b = b0 + threadIdx.x;
-            int v = b < a.n_seqs ? seq_tiles(a, __ldg(a.lens + b)).n * per_seq : 0;
-            int incl = v;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int up = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += up;
-            }
-            if (lane == 31) warp_sum[warp] = incl;
-            __syncthreads();
-            int before = base;
-            for (int w = 0; w < W; ++w) {
-                if (w < warp) before += warp_sum[w];
-                base += warp_sum[w];
-            }
-            if (b < a.n_seqs) plan[b] = before + incl - v;
-            __syncthreads();
-        }
-        if (threadIdx.x == 0) plan[a.n_seqs] = base;
-        __syncthreads();
-    }
-    const int total = plan[a.n_seqs];
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= a.n_seqs; b += W * 32) a.plan[b] = plan[b];
-
-    // rows of the batch without tokens: zeros, or NaN where the length is invalid
-    for (int b = blockIdx.x; b < a.n_seqs; b += gridDim.x) {
-        if (plan[b + 1] != plan[b]) continue;
-        const bool bad = __ldg(a.lens + b) != 0;
-        const uint16_t fill = bad ? (uint16_t)(BF ? 0x7fc0 : 0x7e00) : (uint16_t)0;
-        for (int i = threadIdx.x; i < a.Hq * a.d; i += W * 32) a.out[(int64_t)b * a.Hq * a.d + i] = fill;
-        for (int i = threadIdx.x; i < a.Hq; i += W * 32) {
-            const float l = bad ? NAN : -INFINITY;
-            a.row_lse[(int64_t)b * a.Hq + i] = l;
-            if (a.lse) a.lse[(int64_t)b * a.Hq + i] = l;
-        }
-    }
-
-    const int C = working_ctas(a, total), cta = blockIdx.x;
-    const int run0 = cta < C ? run_begin(total, C, cta) : total, run1 = cta < C ? run_begin(total, C, cta + 1) : total;
-    const int w0 = run0 + run_begin(run1 - run0, W, warp), w1 = run0 + run_begin(run1 - run0, W, warp + 1);
-
-    if (w0 < w1) {
-        unsigned char *my_ring = ring + (size_t)warp * a.stages * S::kStage;
-        const uint32_t ring_addr = smem_u32(my_ring);
-        // ---- feeding: lane i asks for piece i of a tile
-        Cursor pc;
-        pc.start(a, plan, w0);
-        int issued = w0, stage_in = 0;
-        uint32_t poisoned = 0;                                // stages whose tile has a slot outside the pool
-        const int n_pieces = kTile / a.piece;
-        int p_tok, p_slot = 0;
-        bool p_need;
-        auto look_up = [&] {                                  // slot of this lane's piece of the tile that is asked for next
-            p_tok = (pc.s.tile0 + pc.tile) * kTile + lane * a.piece;
-            p_need = lane < n_pieces && p_tok < pc.s.len && p_tok + a.piece > pc.s.first;
-            if (p_need) p_slot = __ldg(a.table + (int64_t)pc.b * a.table_stride + p_tok / a.chunk_len);
-        };
-        auto issue = [&] {
-            const bool inside = p_need && (unsigned)p_slot < (unsigned)a.n_slots;
-            const uint32_t ok = __ballot_sync(0xffffffffu, inside), bad = __ballot_sync(0xffffffffu, p_need && !inside);
-            unsigned long long *bar = &full[stage_in];
-            poisoned = (poisoned & ~(1u << stage_in)) | (bad ? 1u << stage_in : 0u);
-            if (lane == 0) mbar_expect_tx(bar, __popc(ok) * a.piece * 128 * DB * 2);
-            __syncwarp();
-            if (inside) {
-                const int row = p_slot * a.chunk_len + p_tok % a.chunk_len, h = pc.hb / a.blocks;
-                const uint32_t dst = ring_addr + stage_in * S::kStage + lane * a.piece * 128;
-#pragma unroll
-                for (int i = 0; i < DB; ++i) {
-                    tma_load_3d(dst + i * kTile * 128, &map_k, i * 64, row, h, bar);
-                    tma_load_3d(dst + S::kHalf + i * kTile * 128, &map_v, i * 64, row, h, bar);
-                }
-            }
-            ++issued;
-            stage_in = stage_in + 1 == a.stages ? 0 : stage_in + 1;
-            if (issued < w1) {
-                pc.next(a);
-                look_up();
-            }
-        };
-        look_up();
-        for (int s = 0; s < a.stages && issued < w1; ++s) issue();
-
-        // ---- the arithmetic
-        Cursor cc;
-        cc.start(a, plan, w0);
-        uint32_t qf[KS][NT][2];
-        float o[KS][NT][4];
-        float m[NT][2], l[NT][2];
-        int stage = 0, phase = 0;
-        bool fresh = true;
-        // addresses inside a tile: K as stored (rows = tokens), V transposed (rows = channels)
-        const int k_row = lane & 15, v_row = (lane & 7) + ((lane >> 4) << 3);
-        const uint32_t k_base = k_row * 128, v_base = v_row * 128;
-        const uint32_t k_c = lane >> 4, v_c = (lane >> 3) & 1, k_x = k_row & 7, v_x = v_row & 7;
-
-        for (int idx = w0; idx < w1; ++idx) {
-            const int h = cc.hb / a.blocks, rb = cc.hb - h * a.blocks;
-            if (fresh) {
-                fresh = false;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int r = rb * 8 * NT + nt * 8 + (lane >> 2);
-                    const uint16_t *q = a.q + cc.b * a.q_stride + (int64_t)(h * a.group + r) * a.d + (lane & 3) * 2;
-#pragma unroll
-                    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int c = ks * 16 + i * 8;
-                            qf[ks][nt][i] = r < a.group && c + (lane & 3) * 2 < a.d ? __ldg(reinterpret_cast<const uint32_t *>(q + c)) : 0u;
-                        }
-                    m[nt][0] = m[nt][1] = -INFINITY;
-                    l[nt][0] = l[nt][1] = 0.0f;
-#pragma unroll
-                    for (int t = 0; t < KS; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[t][nt][i] = 0.0f;
-                }
-            }
-            const int tok0 = (cc.s.tile0 + cc.tile) * kTile;
-            const uint32_t k_tile = ring_addr + stage * S::kStage, v_tile = k_tile + S::kHalf;
-            const bool poison = !mbar_wait(&full[stage], phase, &gave_up) || (poisoned >> stage & 1);
-
-            const bool newest = a.k_new && tok0 + kTile >= cc.s.len;
-            const bool edge = tok0 < cc.s.first || tok0 + kTile > cc.s.len;
-            if (newest || edge) {
-                // rows that are not seen: V is cleared, so that 0 * (whatever lies there) is 0.  The newest token's row:
-                // what the caller gave, here and in the pool
-                unsigned char *v_mem = my_ring + stage * S::kStage + S::kHalf;
-                if (edge)
-                    for (int i = lane; i < DB * kTile * 8; i += 32) {
-                        const int t = tok0 + (i >> 3) % kTile;
-                        if (t < cc.s.first || t >= cc.s.len) *reinterpret_cast<uint4 *>(v_mem + i * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                if (newest) {
-                    const int t = cc.s.len - 1, r = t - tok0;
-                    const int slot = __ldg(a.table + (int64_t)cc.b * a.table_stride + t / a.chunk_len);
-                    const bool inside = (unsigned)slot < (unsigned)a.n_slots;
-                    const int64_t at = (int64_t)h * a.stride_h + ((int64_t)slot * a.chunk_len + t % a.chunk_len) * a.d;
-                    const int64_t from = cc.b * a.new_stride + (int64_t)h * a.d;
-                    for (int c = lane; c < a.d / 8; c += 32) {
-                        const uint4 kn = __ldg(reinterpret_cast<const uint4 *>(a.k_new + from) + c);
-                        const uint4 vn = __ldg(reinterpret_cast<const uint4 *>(a.v_new + from) + c);
-                        unsigned char *mem = v_mem + (c >> 3) * kTile * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-                        *reinterpret_cast<uint4 *>(mem - S::kHalf) = kn;
-                        *reinterpret_cast<uint4 *>(mem) = vn;
-                        if (inside && rb == 0) {
-                            reinterpret_cast<uint4 *>(a.k + at)[c] = kn;
-                            reinterpret_cast<uint4 *>(a.v + at)[c] = vn;
-                        }
-                    }
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // before TMA fills this stage again
-                __syncwarp();
-            }
-
-            // logits: tokens x query rows, two chains of accumulators
-            float s[NT][4], s2[NT][4];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[nt][i] = s2[nt][i] = 0.0f;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                uint32_t f[4];
-                const uint32_t c = (ks & 3) * 2 + k_c;
-                ldsm4(f, k_tile + (ks >> 2) * kTile * 128 + k_base + ((c ^ k_x) << 4));
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<BF>(ks & 1 ? s2[nt] : s[nt], f, qf[ks][nt][0], qf[ks][nt][1]);
-            }
-            uint32_t p_hi[NT][2], p_lo[NT][2];
-            bool moved = false;
-            float keep[NT][2];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float v[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[i] = (s[nt][i] + s2[nt][i]) * a.scale_log2;
-                    if (poison) v[i] = NAN;
-                }
-                if (edge) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int t = tok0 + (lane >> 2) + (i >> 1) * 8;
-                        if (t < cc.s.first || t >= cc.s.len) v[i] = -INFINITY;
-                    }
-                }
-                if (a.logits) {
-                    const int r0 = rb * 8 * NT + nt * 8 + (lane & 3) * 2;
-                    float *to = a.logits + (((int64_t)cc.b * a.Hkv + h) * a.max_len + tok0) * a.group + r0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int t = (lane >> 2) + (i >> 1) * 8;
-                        if (r0 + (i & 1) < a.group && tok0 + t < cc.s.len) to[(int64_t)t * a.group + (i & 1)] = v[i];
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float top = fmaxf(v[i], v[i + 2]);
-#pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                    top = fmaxf(top, m[nt][i]);
-                    const float ref = top == -INFINITY ? 0.0f : top;
-                    keep[nt][i] = top == m[nt][i] ? 1.0f : exp2_fast(m[nt][i] - ref);
-                    moved |= top != m[nt][i];
-                    m[nt][i] = top;
-                    v[i] = exp2_fast(v[i] - ref);
-                    v[i + 2] = exp2_fast(v[i + 2] - ref);
-                    l[nt][i] = __fmaf_rn(l[nt][i], keep[nt][i], v[i] + v[i + 2]);
-                }
-                constexpr float kCut = kLift * (BF ? 1.0f - 1.0f / 512.0f : 1.0f - 1.0f / 4096.0f);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t hi = pack_cut<BF>(v[2 * i] * kCut, v[2 * i + 1] * kCut);
-                    const float2 back = unpack<BF>(hi);
-                    const uint32_t lo = pack_round<BF>(__fmaf_rn(v[2 * i], kLift, -back.x), __fmaf_rn(v[2 * i + 1], kLift, -back.y));
-                    p_hi[nt][i] = transpose8x8(hi);
-                    p_lo[nt][i] = transpose8x8(lo);
-                }
-            }
-            if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-                for (int t = 0; t < KS; ++t)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[t][nt][i] *= keep[nt][i & 1];
-            }
-#pragma unroll
-            for (int t = 0; t < KS; ++t) {
-                uint32_t f[4];
-                const uint32_t c = (t & 3) * 2 + v_c;
-                ldsm4_trans(f, v_tile + (t >> 2) * kTile * 128 + v_base + ((c ^ v_x) << 4));
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    mma<BF>(o[t][nt], f, p_hi[nt][0], p_hi[nt][1]);
-                    mma<BF>(o[t][nt], f, p_lo[nt][0], p_lo[nt][1]);
-                }
-            }
-            __syncwarp();
-            if (issued < w1) issue();
-            if (++stage == a.stages) {
-                stage = 0;
-                phase ^= 1;
-            }
-
-            // the end of the item, or of this warp's run
-            const bool item_ends = cc.tile + 1 == cc.s.n;
-            if (item_ends || idx + 1 == w1) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], d);
-                const int item_begin = idx - cc.tile;
-                if (item_ends && item_begin >= w0) {
-                    // complete: to the output, two channels of a row per lane
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        float inv[2];
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) inv[i] = l[nt][i] == 0.0f ? 0.0f : (1.0f / kLift) / l[nt][i];
-                        const int r = rb * 8 * NT + nt * 8 + (lane >> 2);
-                        uint16_t *to = a.out + ((int64_t)cc.b * a.Hq + h * a.group + r) * a.d + (lane & 3) * 2;
-#pragma unroll
-                        for (int t = 0; t < KS; ++t)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const uint32_t x = transpose8x8(pack_round<BF>(o[t][nt][2 * i] * inv[0], o[t][nt][2 * i + 1] * inv[1]));
-                                if (r < a.group && t * 16 + i * 8 + (lane & 3) * 2 < a.d) *reinterpret_cast<uint32_t *>(to + t * 16 + i * 8) = x;
-                            }
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int r2 = rb * 8 * NT + nt * 8 + (lane & 3) * 2 + i;
-                            if (lane < 4 && r2 < a.group) {
-                                const int64_t at = (int64_t)cc.b * a.Hq + h * a.group + r2;
-                                const float lg = l[nt][i] == 0.0f ? -INFINITY : m[nt][i] + log2f(l[nt][i]);
-                                a.row_lse[at] = lg;
-                                if (a.lse) a.lse[at] = lg * kLn2;
-                            }
-                        }
-                    }
-                } else {
-                    // a piece: the run's last one, unless the item ends here (then it began before the run)
-                    const int which = item_ends ? 0 : 1;
-                    float *to = which == 0 ? first_pieces + warp * piece_floats<DB>(a.rows) : reinterpret_cast<float *>(my_ring);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int r = nt * 8 + (lane & 3) * 2 + (i & 1);
-                            if (r < a.rows) {
-#pragma unroll
-                                for (int t = 0; t < KS; ++t) to[r * S::kPitch + t * 16 + (i >> 1) * 8 + (lane >> 2)] = o[t][nt][i];
-                                if (lane < 4 && i < 2) {
-                                    to[r * S::kPitch + S::kCols] = m[nt][i];
-                                    to[r * S::kPitch + S::kCols + 1] = l[nt][i];
-                                }
-                            }
-                        }
-                    if (lane == 0) {
-                        piece_item[2 * warp + which] = cc.b * per_seq + cc.hb;
-                        piece_at[2 * warp + which] = item_begin;
-                    }
-                }
-                fresh = true;
-            }
-            cc.next(a);
-        }
-    }
-    __syncthreads();
-    grid_launch_dependents();
-
-    // ---- the pieces that the warps left: runs of pieces of one item, joined; all threads share the elements
-    const int row_elems = S::kCols;
-    for (int p = 0; p < 2 * W;) {
-        const int item = piece_item[p];
-        if (item < 0) {
-            ++p;
-            continue;
-        }
-        int end = p + 1;
-        while (end < 2 * W && (piece_item[end] == item || piece_item[end] < 0)) ++end;
-        const int b = item / per_seq, hb = item - b * per_seq, h = hb / a.blocks, rb = hb - h * a.blocks;
-        const int begin = piece_at[p], finish = begin + (plan[b + 1] - plan[b]) / per_seq;
-        const bool whole = begin >= run0 && finish <= run1;
-        float *part = a.part + ((int64_t)cta * 2 + (begin < run0 ? 0 : 1)) * a.rows * (S::kCols + 2);
-        for (int e = threadIdx.x; e < a.rows * row_elems; e += W * 32) {
-            const int r = e / row_elems, c = e - r * row_elems;
-            if (rb * 8 * NT + r >= a.group) continue;
-            float top = -INFINITY;
-            for (int i = p; i < end; ++i) {
-                if (piece_item[i] < 0) continue;
-                const float *at = i & 1 ? reinterpret_cast<const float *>(ring + (size_t)(i >> 1) * a.stages * S::kStage)
-                                        : first_pieces + (i >> 1) * piece_floats<DB>(a.rows);
-                top = fmaxf(top, at[r * S::kPitch + S::kCols]);
-            }
-            const float ref = top == -INFINITY ? 0.0f : top;
-            float sum = 0.0f, acc = 0.0f;
-            for (int i = p; i < end; ++i) {
-                if (piece_item[i] < 0) continue;
-                const float *at = i & 1 ? reinterpret_cast<const float *>(ring + (size_t)(i >> 1) * a.stages * S::kStage)
-                                        : first_pieces + (i >> 1) * piece_floats<DB>(a.rows);
-                const float f = exp2_fast(at[r * S::kPitch + S::kCols] - ref);
-                sum = __fmaf_rn(f, at[r * S::kPitch + S::kCols + 1], sum);
-                acc = __fmaf_rn(f, at[r * S::kPitch + c], acc);
-            }
-            if (whole) {
-                const int64_t row = (int64_t)b * a.Hq + h * a.group + rb * 8 * NT + r;
-                if (c < a.d) {
-                    const float x = sum == 0.0f ? 0.0f : acc * (1.0f / kLift) / sum;
-                    a.out[row * a.d + c] = (uint16_t)pack_round<BF>(x, x);
-                }
-                if (c == 0) {
-                    const float lg = sum == 0.0f ? -INFINITY : top + log2f(sum);
-                    a.row_lse[row] = lg;
-                    if (a.lse) a.lse[row] = lg * kLn2;
-                }
-            } else {
-                part[(int64_t)r * (S::kCols + 2) + c] = acc;
-                if (c < 2) part[(int64_t)r * (S::kCols + 2) + S::kCols + c] = c == 0 ? top : sum;
-            }
-        }
-        p = end;
-    }
-}
-
-// Items that span CTAs: block (c, r) joins query row r of the item that begins in CTA c's run and goes on behind it (if one
-// does), threads over channels and, where there are many pieces, over them.
-constexpr int kJoinThreads = 256;
+// Four channels of a finished row (16-bit values), and with the first ones the row's log-sum.
 template <bool BF>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const DecodeArgs a, int cols)
+__device__ __forceinline__ void finish_row(const DecodeArgs &a, int64_t row, int c, const float (&acc)[4], float top, float sum)
 {
-    __shared__ float s_acc[kJoinThreads], s_top[kJoinThreads / 32], s_sum[kJoinThreads / 32];
-    grid_dependency_wait();
-    const int per_seq = a.Hkv * a.blocks, c0 = blockIdx.x, r = blockIdx.y;
-    const int total = a.plan[a.n_seqs], C = working_ctas(a, total);
-    if (c0 + 1 >= C) return;
-    const int begin_run = run_begin(total, C, c0), border = run_begin(total, C, c0 + 1);
-    Cursor last;                                              // the run's last tile
-    last.start(a, a.plan, border - 1);
-    const int b = last.b, h = last.hb / a.blocks, rb = last.hb - h * a.blocks, row_in_group = rb * a.rows + r;
-    const int begin = border - 1 - last.tile, tiles = last.s.n;
-    if (begin < begin_run || begin + tiles <= border || row_in_group >= a.group) return;
-    const int c1 = run_of(total, C, begin + tiles - 1);
-    const int64_t stride = (int64_t)a.rows * (cols + 2);
-    const float *base = a.part + (int64_t)r * (cols + 2);
-    // first CTA's last piece, then the following CTAs' first pieces
-    auto at = [&](int c) { return base + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * stride; };
-    float top = -INFINITY;
-    for (int c = c0 + threadIdx.x; c <= c1; c += kJoinThreads) top = fmaxf(top, at(c)[cols]);
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
-    __syncthreads();
-    for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, s_top[w]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
-    for (int c = c0 + threadIdx.x; c <= c1; c += kJoinThreads) sum = __fmaf_rn(exp2_fast(at(c)[cols] - ref), at(c)[cols + 1], sum);
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    sum = 0.0f;
-    for (int w = 0; w < kJoinThreads / 32; ++w) sum += s_sum[w];
-    const int slices = kJoinThreads / cols, slice = threadIdx.x / cols, col = threadIdx.x - slice * cols;
-    float acc = 0.0f;
-    if (slice < slices)
-        for (int c = c0 + slice; c <= c1; c += slices) acc = __fmaf_rn(exp2_fast(at(c)[cols] - ref), at(c)[col], acc);
-    s_acc[threadIdx.x] = acc;
-    __syncthreads();
-    const int64_t row = (int64_t)b * a.Hq + h * a.group + row_in_group;
-    if (slice == 0 && col < a.d) {
-        for (int i = 1; i < slices; ++i) acc += s_acc[i * cols + col];
-        const float x = sum == 0.0f ? 0.0f : acc * (1.0f / kLift) / sum;
-        a.out[row * a.d + col] = (uint16_t)pack_round<BF>(x, x);
+    const float inv = sum == 0.0f ? 0.0f : (1.0f / kLift) / sum;
+    if (c < a.d) {
+        const uint2 x = make_uint2(pack_round<BF>(acc[0] * inv, acc[1] * inv), pack_round<BF>(acc[2] * inv, acc[3] * inv));
+        *reinterpret_cast<uint2 *>(a.out + row * a.d + c) = x;
     }
-    if (threadIdx.x == 0) {
+    if (c == 0) {
         const float lg = sum == 0.0f ? -INFINITY : top + log2f(sum);
         a.row_lse[row] = lg;
         if (a.lse) a.lse[row] = lg * kLn2;
     }
 }
 
-// Weights of all tokens: the logits left by the main kernel against the rows' log-sums.
-__global__ void __launch_bounds__(256) mass_kernel(const DecodeArgs a)
+template <int DB> struct DecodeShape {
+    static constexpr int kStages = DB == 1 ? 4 : 2;
+    static constexpr int kHalf = DB * kTile * 128;            // K (or V) of a tile
+    static constexpr int kStage = 2 * kHalf;
+    static constexpr int kCols = DB * 64;                     // channels, rounded up to whole boxes
+    static constexpr int kPitch = kCols + 4;                  // floats per row of a partial result: O, then m and l
+};
+
+// Shared memory: [1 KiB alignment][stages x tile][query rows of two items].
+//
+// MODE: up to 4, 8 or 16 query rows.  With up to 4 the MMA's eight columns hold every row twice: the second copy's lanes
+// turn their weights into the lo parts, so hi and lo take one MMA together and the copies' results are added at the end.
+template <bool BF, int DB, int MODE>
+__global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap map)
 {
+    constexpr int NT = MODE == 2 ? 2 : 1;                     // column groups of eight query rows
+    constexpr bool kTwin = MODE == 0;
+    using S = DecodeShape<DB>;
+    constexpr int KS = DB * 4;                                // k-steps over the channels; also 16-channel tiles of the output
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const uint32_t ring_addr = smem_u32(ring), q_addr = ring_addr + S::kStages * S::kStage;
+    __shared__ unsigned long long full[S::kStages];
+    __shared__ uint32_t gave_up;
+
+    const int lane = threadIdx.x, run = blockIdx.x;
+    if (lane == 0) {
+#pragma unroll
+        for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        gave_up = 0;
+    }
+    __syncwarp();
     grid_dependency_wait();
-    const int b = blockIdx.z, h = blockIdx.y, n = __ldg(a.lens + b), t = blockIdx.x * 256 + threadIdx.x;
-    if (n > a.max_len || t >= n) return;
-    const int first = a.window > 0 && n > a.window ? n - a.window : 0;
-    const int64_t at = (int64_t)b * a.Hkv + h;
-    float w = 0.0f;
-    if (t >= first) {
-        const float *v = a.logits + (at * a.max_len + t) * a.group, *l = a.row_lse + at * a.group;
-        for (int g = 0; g < a.group; ++g) {
-            const float lg = l[g];
-            w += lg == -INFINITY ? 0.0f : exp2_fast(v[g] - lg);
+    grid_launch_dependents();
+
+    // tiles of the batch, and the sequence that this run begins in: a lane adds up neighbouring sequences
+    const int per_seq = a.Hkv * a.blocks, each = (a.n_seqs + 31) / 32;
+    int incl = 0;
+    for (int b = lane * each; b < min(a.n_seqs, (lane + 1) * each); ++b) incl += seq_tiles(a, __ldg(a.lens + b)).n * per_seq;
+    const int own = incl;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += up;
+    }
+    const int total = __shfl_sync(0xffffffffu, incl, 31);
+    const int runs = working_runs(a, total);
+    const int w0 = run < runs ? run_begin(total, runs, run) : 0, w1 = run < runs ? run_begin(total, runs, run + 1) : 0;
+    int open_item = -1;                                       // the item that begins in this run and goes on behind it
+
+    if (w0 < w1) {
+        const int holder = __ffs(__ballot_sync(0xffffffffu, incl > w0)) - 1;
+        int f_seq = holder * each, f_base = __shfl_sync(0xffffffffu, incl - own, holder);   // a sequence, and its first tile
+        SeqTiles f_s = seq_tiles(a, __ldg(a.lens + f_seq));
+        auto skip = [&](int idx) {                            // on to the sequence that has tile idx
+            while (f_base + f_s.n * per_seq <= idx) {
+                f_base += f_s.n * per_seq;
+                f_s = seq_tiles(a, __ldg(a.lens + ++f_seq));
+            }
+        };
+        skip(w0);
+        int c_seq = f_seq, c_hb = (w0 - f_base) / f_s.n, c_tile = w0 - f_base - c_hb * f_s.n;   // where the arithmetic is
+        SeqTiles c_s = f_s;
+
+        // ---- feeding: lane i looks up piece i % n_pieces of the tile i / n_pieces behind `base`
+        const int n_pieces = kTile / a.piece, ahead = a.piece * 2;            // pieces per tile, tiles per look-up
+        int f_row, f_slot, f_q;                                               // row in its chunk, slot, sequence
+        bool f_need;
+        uint32_t f_h, f_qb;                                                   // KV head (and first query row << 16); bytes of query rows,
+                                                                              // which come with the first tile of an item
+        auto look_up = [&](int base) {
+            const int idx = base + lane / n_pieces, last = min(base + ahead, w1) - 1;
+            f_need = false;
+            f_slot = -1;
+            f_qb = 0;
+            for (;;) {
+                if (idx >= f_base && idx <= last && idx < f_base + f_s.n * per_seq) {
+                    const int hb = (idx - f_base) / f_s.n, tile = idx - f_base - hb * f_s.n;
+                    const int tok = (f_s.tile0 + tile) * kTile + (lane & (n_pieces - 1)) * a.piece;
+                    f_need = tok < f_s.len && tok + a.piece > f_s.first;
+                    f_h = hb / a.blocks;
+                    const int chunk = tok / a.chunk_len;
+                    f_row = tok - chunk * a.chunk_len;
+                    if (f_need) f_slot = __ldg(a.table + (int64_t)f_seq * a.table_stride + chunk);
+                    if ((idx == w0 || tile == 0) && (lane & (n_pieces - 1)) == 0) {
+                        const int r0 = (hb - f_h * a.blocks) * 8 * NT;
+                        f_qb = min(a.rows, a.group - r0) * a.d * 2;
+                        f_q = f_seq;
+                        f_h |= (uint32_t)r0 << 16;
+                    }
+                }
+                if (last < f_base + f_s.n * per_seq) break;
+                skip(f_base + f_s.n * per_seq);
+            }
+        };
+        int base = w0, issued = w0, stage_in = 0, q_issued = 0, q_read = 0;
+        uint32_t ok_mask = 0, bad_mask = 0, q_mask = 0, poisoned = 0;         // poisoned: stages whose tile has a slot outside the pool
+        bool fetched = false;                                                 // the masks belong to the look-up at `base`
+        auto issue = [&] {
+            if (!fetched) {
+                const bool inside = f_need && (unsigned)f_slot < (unsigned)a.n_slots;
+                ok_mask = __ballot_sync(0xffffffffu, inside);
+                bad_mask = __ballot_sync(0xffffffffu, f_need && !inside);
+                q_mask = __ballot_sync(0xffffffffu, f_qb != 0);
+                fetched = true;
+            }
+            const int lead = (issued - base) * n_pieces;
+            const bool with_q = q_mask >> lead & 1;
+            if (with_q && q_issued - q_read >= kQuerySlots) return;           // its query rows have no place yet
+            const uint32_t mine = ((1u << n_pieces) - 1u) << lead;
+            unsigned long long *bar = &full[stage_in];
+            poisoned = (poisoned & ~(1u << stage_in)) | (bad_mask & mine ? 1u << stage_in : 0u);
+            if (lane == lead) mbar_expect_tx(bar, __popc(ok_mask & mine) * a.piece * 128 * DB * 2 + f_qb);
+            __syncwarp();
+            if (mine >> lane & 1) {
+                if (ok_mask >> lane & 1) {
+                    const int row = f_slot * a.chunk_len + f_row, h = f_h & 0xffff;
+                    const uint32_t dst = ring_addr + stage_in * S::kStage + (lane - lead) * a.piece * 128;
+                    if (a.whole_tile) {
+                        tma_load_5d(dst, &map, 0, row, 0, h, 0, bar);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < DB; ++i) {
+                            tma_load_5d(dst + i * kTile * 128, &map, i * 64, row, 0, h, 0, bar);
+                            tma_load_5d(dst + S::kHalf + i * kTile * 128, &map, i * 64, row, 0, h, 1, bar);
+                        }
+                    }
+                }
+                if (f_qb)
+                    bulk_load(q_addr + (q_issued % kQuerySlots) * a.q_bytes,
+                              a.q + f_q * a.q_stride + (int64_t)((f_h & 0xffff) * a.group + (f_h >> 16)) * a.d, f_qb, bar);
+            }
+            q_issued += with_q;
+            ++issued;
+            stage_in = stage_in + 1 == S::kStages ? 0 : stage_in + 1;
+            if (issued - base == ahead && issued < w1) {
+                base = issued;
+                fetched = false;
+                look_up(base);
+            }
+        };
+        look_up(base);
+#pragma unroll 1
+        for (int s = 0; s < S::kStages && issued < w1; ++s) issue();
+
+        // ---- the arithmetic
+        int stage = 0, phase = 0, done = w0;
+        // addresses inside a tile: K as stored (rows = tokens), V transposed (rows = channels)
+        const int k_row = lane & 15, v_row = (lane & 7) + ((lane >> 4) << 3);
+        const uint32_t k_base = ring_addr + k_row * 128, v_base = ring_addr + S::kHalf + v_row * 128;
+        const uint32_t k_c = lane >> 4, v_c = (lane >> 3) & 1, k_x = k_row & 7, v_x = v_row & 7;
+
+#pragma unroll 1
+        for (int idx = w0; idx < w1;) {                       // the items that this run has tiles of
+            const int h = c_hb / a.blocks, rb = c_hb - h * a.blocks;
+            const int row0 = rb * 8 * NT, have = min(a.rows, a.group - row0);     // query rows of this item
+            const int tile_end = min(c_s.n, c_tile + w1 - idx);
+            const bool item_ends = tile_end == c_s.n;
+            // the newest token's row, for the item's last tile: lanes hold 16 bytes each of K (first) and V
+            uint4 fresh[DB <= 2 ? 1 : 2];
+            int fresh_slot = -1;
+            const bool append = a.k_new && item_ends;
+            if (append) {
+#pragma unroll
+                for (int i = 0; i < (DB <= 2 ? 1 : 2); ++i) {
+                    const int c = lane + i * 32, half = a.d / 8;
+                    const uint16_t *from = c < half ? a.k_new : a.v_new;
+                    if (c < 2 * half) fresh[i] = __ldg(reinterpret_cast<const uint4 *>(from + c_seq * a.new_stride + (int64_t)h * a.d) + (c < half ? c : c - half));
+                }
+                fresh_slot = __ldg(a.table + (int64_t)c_seq * a.table_stride + (c_s.len - 1) / a.chunk_len);
+            }
+            bool good = mbar_wait(&full[stage], phase, &gave_up);
+            // query rows as the MMA's second operand; columns beyond the item's rows repeat others (nobody reads their
+            // results), channels behind head_dim are 0 like K's there
+            uint32_t qf[KS][NT][2];
+            float o[KS][NT][4], ref[NT][2], limit[NT][2], l[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int r = nt * 8 + (lane & (kTwin ? 3 : 7));
+                const uint32_t row = q_addr + (q_read % kQuerySlots) * a.q_bytes + min(r, have - 1) * a.d * 2;
+#pragma unroll
+                for (int ks = 0; ks < KS; ks += 2) {
+                    uint32_t f[4];
+                    const int c = ks * 16 + (lane >> 3) * 8;
+                    ldsm4(f, row + (c < a.d ? c * 2 : 0));
+                    qf[ks][nt][0] = ks * 16 < a.d ? f[0] : 0u;
+                    qf[ks][nt][1] = ks * 16 < a.d ? f[1] : 0u;
+                    qf[ks + 1][nt][0] = ks * 16 + 16 < a.d ? f[2] : 0u;
+                    qf[ks + 1][nt][1] = ks * 16 + 16 < a.d ? f[3] : 0u;
+                }
+                ref[nt][0] = ref[nt][1] = 0.0f;
+                limit[nt][0] = limit[nt][1] = -INFINITY;      // reference + kSlack; -inf: no logit yet
+                l[nt][0] = l[nt][1] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < KS; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[t][nt][i] = 0.0f;
+            }
+            __syncwarp();
+            ++q_read;
+            float *logits = nullptr;
+            if (a.logits) logits = a.logits + ((int64_t)c_seq * a.Hkv + h) * a.max_len * a.group + row0 + (lane & 3) * 2;
+            const int tile_begin = c_tile;
+
+#pragma unroll 1
+            for (int tile = tile_begin; tile < tile_end; ++tile) {
+                if (tile != tile_begin) good = mbar_wait(&full[stage], phase, &gave_up);
+                const int tok0 = (c_s.tile0 + tile) * kTile;
+                const uint32_t at = stage * S::kStage;
+                const bool poison = !good || (poisoned >> stage & 1);
+                // tiles that hold places nobody sees, the newest token, or a slot outside the pool
+                const bool special = poison || tok0 < c_s.first || tok0 + kTile > c_s.len || (append && tile + 1 == c_s.n);
+                if (special) {
+                    // rows that are not seen: V is cleared, so that 0 * (whatever lies there) is 0.  The newest token's row:
+                    // what the caller gave, here and in the pool
+                    unsigned char *mem = ring + at;
+#pragma unroll 1
+                    for (int i = lane; i < DB * kTile * 8; i += 32) {
+                        const int t = tok0 + (i >> 3) % kTile;
+                        if (t < c_s.first || t >= c_s.len) *reinterpret_cast<uint4 *>(mem + S::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    if (append && tile + 1 == c_s.n) {
+                        const int t = c_s.len - 1, r = t - tok0;
+                        const bool inside = (unsigned)fresh_slot < (unsigned)a.n_slots && rb == 0;
+                        const int64_t to = (int64_t)h * a.stride_h + ((int64_t)fresh_slot * a.chunk_len + t % a.chunk_len) * a.d;
+#pragma unroll
+                        for (int i = 0; i < (DB <= 2 ? 1 : 2); ++i) {
+                            const int half = a.d / 8, cv = lane + i * 32, c = cv < half ? cv : cv - half;
+                            if (cv < 2 * half) {
+                                *reinterpret_cast<uint4 *>(mem + (cv < half ? 0 : S::kHalf) + (c >> 3) * kTile * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = fresh[i];
+                                if (inside) reinterpret_cast<uint4 *>((cv < half ? a.k : a.v) + to)[c] = fresh[i];
+                            }
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // before TMA fills this stage again
+                    __syncwarp();
+                }
+
+                // logits: tokens x query rows, two chains of accumulators
+                float s[NT][4], s2[NT][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[nt][i] = s2[nt][i] = 0.0f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    uint32_t f[4];
+                    ldsm4(f, k_base + at + (ks >> 2) * kTile * 128 + ((((ks & 3) * 2 + k_c) ^ k_x) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma<BF>(ks & 1 ? s2[nt] : s[nt], f, qf[ks][nt][0], qf[ks][nt][1]);
+                }
+                bool over = false;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[nt][i] = (s[nt][i] + s2[nt][i]) * a.scale_log2;
+                if (special) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int t = tok0 + (lane >> 2) + (i >> 1) * 8;
+                            if (poison) s[nt][i] = NAN;
+                            if (t < c_s.first || t >= c_s.len) s[nt][i] = -INFINITY;
+                        }
+                }
+                if (logits) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int t = tok0 + (lane >> 2) + (i >> 1) * 8;
+                            if (nt * 8 + (lane & 3) * 2 + (i & 1) < have && t < c_s.len) logits[(int64_t)t * a.group + nt * 8 + (i & 1)] = s[nt][i];
+                        }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) over |= s[nt][i] > limit[nt][i & 1];
+                if (__any_sync(0xffffffffu, over)) {          // the references move up to the maxima
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float top = fmaxf(s[nt][i], s[nt][i + 2]);
+#pragma unroll
+                            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                            if (top > limit[nt][i] - kSlack) {
+                                const float keep = limit[nt][i] == -INFINITY ? 0.0f : exp2_fast(ref[nt][i] - top);
+                                ref[nt][i] = top;
+                                limit[nt][i] = top + kSlack;
+                                l[nt][i] *= keep;
+#pragma unroll
+                                for (int t = 0; t < KS; ++t) {
+                                    o[t][nt][i] *= keep;
+                                    o[t][nt][i + 2] *= keep;
+                                }
+                            }
+                        }
+                }
+                constexpr float kCut = kLift * (BF ? 1.0f - 1.0f / 512.0f : 1.0f - 1.0f / 4096.0f);
+                uint32_t p_hi[NT][2], p_lo[NT][2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[nt][i] = exp2_fast(s[nt][i] - ref[nt][i & 1]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        l[nt][i] += s[nt][i] + s[nt][i + 2];
+                        const uint32_t hi = pack_cut<BF>(s[nt][2 * i] * kCut, s[nt][2 * i + 1] * kCut);
+                        const float2 back = unpack<BF>(hi);
+                        const uint32_t lo = pack_round<BF>(__fmaf_rn(s[nt][2 * i], kLift, -back.x), __fmaf_rn(s[nt][2 * i + 1], kLift, -back.y));
+                        p_hi[nt][i] = transpose8x8(kTwin && (lane & 2) ? lo : hi);
+                        if constexpr (!kTwin) p_lo[nt][i] = transpose8x8(lo);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < KS; ++t) {
+                    uint32_t f[4];
+                    ldsm4_trans(f, v_base + at + (t >> 2) * kTile * 128 + ((((t & 3) * 2 + v_c) ^ v_x) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        mma<BF>(o[t][nt], f, p_hi[nt][0], p_hi[nt][1]);
+                        if constexpr (!kTwin) mma<BF>(o[t][nt], f, p_lo[nt][0], p_lo[nt][1]);
+                    }
+                }
+                __syncwarp();
+                ++done;
+#pragma unroll 1
+                for (int s = 0; s < 2 && issued < w1 && issued < done + S::kStages; ++s) issue();   // two: one may have had to wait
+                if (++stage == S::kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+
+            // the end of the item, or of this warp's run
+            const int item_begin = idx - tile_begin;
+            idx += tile_end - tile_begin;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], d);
+            if constexpr (kTwin) {
+#pragma unroll
+                for (int t = 0; t < KS; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[t][0][i] += __shfl_xor_sync(0xffffffffu, o[t][0][i], 2);
+            }
+            if (item_ends && tile_begin == 0) {
+                // complete: to the output, two channels of a row per lane
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float inv[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) inv[i] = l[nt][i] == 0.0f ? 0.0f : (1.0f / kLift) / l[nt][i];
+                    const int r = nt * 8 + (lane >> 2);
+                    uint16_t *to = a.out + ((int64_t)c_seq * a.Hq + h * a.group + row0 + r) * a.d + (lane & 3) * 2;
+#pragma unroll
+                    for (int t = 0; t < KS; ++t)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t x = transpose8x8(pack_round<BF>(o[t][nt][2 * i] * inv[0], o[t][nt][2 * i + 1] * inv[1]));
+                            if (r < have && t * 16 + i * 8 + (lane & 3) * 2 < a.d) *reinterpret_cast<uint32_t *>(to + t * 16 + i * 8) = x;
+                        }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int r2 = nt * 8 + (lane & 3) * 2 + i;
+                        if (lane < 4 && r2 < have) {
+                            const int64_t row = (int64_t)c_seq * a.Hq + h * a.group + row0 + r2;
+                            const float lg = l[nt][i] == 0.0f ? -INFINITY : ref[nt][i] + log2f(l[nt][i]);
+                            a.row_lse[row] = lg;
+                            if (a.lse) a.lse[row] = lg * kLn2;
+                        }
+                    }
+                }
+            } else {
+                // a piece: of an item that began before this run, or of one that goes on behind it
+                float *to = a.part + ((int64_t)run * 2 + (tile_begin > 0 ? 0 : 1)) * a.rows * S::kPitch;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = nt * 8 + (lane & 3) * 2 + (i & 1);
+                        if (r < a.rows) {
+#pragma unroll
+                            for (int t = 0; t < KS; ++t) to[r * S::kPitch + t * 16 + (i >> 1) * 8 + (lane >> 2)] = o[t][nt][i];
+                            if (lane < 4 && i < 2)
+                                *reinterpret_cast<float2 *>(to + r * S::kPitch + S::kCols) =
+                                    make_float2(limit[nt][i] == -INFINITY ? -INFINITY : ref[nt][i], l[nt][i]);
+                        }
+                    }
+            }
+            const int item = c_seq * per_seq + c_hb;
+            if (tile_begin == 0) {                            // the item begins here: say who has its tiles
+                if (!item_ends) open_item = item;
+                if (lane == 0) a.span[item] = item_ends ? make_int2(-1, 0) : make_int2(run, run_of(total, runs, item_begin + c_s.n - 1));
+            }
+            if (idx < w1) {
+                c_tile = 0;
+                if (++c_hb == per_seq) {
+                    c_hb = 0;
+                    do c_s = seq_tiles(a, __ldg(a.lens + ++c_seq));
+                    while (c_s.n == 0);
+                }
+            }
         }
     }
-    a.mass_out[at * a.mass_stride + t] = (a.mass_in ? a.mass_in[at * a.mass_stride + t] : 0.0f) + w;
+    if (lane == 0) a.open[run] = open_item;
+
+    // rows of the batch without tokens: zeros, or NaN where the length is invalid
+    for (int b = run; b < a.n_seqs; b += gridDim.x) {
+        const int len = __ldg(a.lens + b);
+        if (seq_tiles(a, len).n) continue;
+        const uint32_t fill = len ? (BF ? 0x7fc07fc0u : 0x7e007e00u) : 0u;
+        uint4 *to = reinterpret_cast<uint4 *>(a.out + (int64_t)b * a.Hq * a.d);
+#pragma unroll 1
+        for (int i = lane; i < a.Hq * a.d / 8; i += 32) to[i] = make_uint4(fill, fill, fill, fill);
+#pragma unroll 1
+        for (int i = lane; i < a.Hq; i += 32)
+            if (a.lse) a.lse[(int64_t)b * a.Hq + i] = len ? NAN : -INFINITY;
+    }
 }
 
+// Items that span runs are joined, block (x, y) taking kJoinCols groups of four channels of the y-th part of item x (by_item) or of
+// the item that is open at the end of run x, in SLICES over the runs that have pieces of it.  The other blocks: the weights
+// of kMassTokens tokens per thread.
+constexpr int kJoinCols = 16, kMassTokens = 4;
+struct FinishArgs {
+    int by_item, joins, join_y, cols, mass_x;
+};
+
+__device__ __forceinline__ void lse_add(float &top, float &sum, float m, float l)   // (top, sum) joined with (m, l)
+{
+    const float t = fmaxf(top, m), ref = t == -INFINITY ? 0.0f : t;
+    sum = __fmaf_rn(sum, exp2_fast(top - ref), l * exp2_fast(m - ref));
+    top = t;
+}
+
+template <bool BF, int SLICES>
+__global__ void __launch_bounds__(SLICES * kJoinCols) finish_kernel(const DecodeArgs a, const FinishArgs f)
+{
+    constexpr int kThreads = SLICES * kJoinCols;
+    __shared__ float4 s_acc[kThreads];
+    __shared__ float2 s_ml[SLICES];
+    __shared__ float s_lse[64];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int per_seq = a.Hkv * a.blocks, pitch = f.cols + 4, block_rows = a.group > 8 ? 16 : 8;
+    const int64_t stride = (int64_t)a.rows * pitch;
+    if ((int)blockIdx.x < f.joins) {
+        const int x = blockIdx.x / f.join_y, y = blockIdx.x - x * f.join_y;
+        const int item = f.by_item ? x : a.open[x];
+        if (item < 0) return;
+        const int b = item / per_seq, hb = item - b * per_seq, h = hb / a.blocks, rb = hb - h * a.blocks;
+        const int2 span = a.span[item];
+        if (f.by_item && seq_tiles(a, __ldg(a.lens + b)).n == 0) return;   // its span was never written
+        if (span.x < 0) return;
+        const int slice = threadIdx.x / kJoinCols, e = y * kJoinCols + threadIdx.x % kJoinCols;
+        const int r = e / (f.cols / 4), c = (e - r * (f.cols / 4)) * 4;     // one row per block: cols / 4 is a multiple of kJoinCols
+        if (rb * block_rows + r >= a.group) return;
+        float top = -INFINITY, sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float *from = a.part + (int64_t)r * pitch;
+#pragma unroll 4
+        for (int i = span.x + slice; i <= span.y; i += SLICES) {
+            // the first run's last piece, then the following runs' first ones
+            const float *at = from + ((int64_t)i * 2 + (i == span.x)) * stride;
+            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(at + f.cols));
+            const float4 v = __ldcg(reinterpret_cast<const float4 *>(at + c));
+            const float t = fmaxf(top, ml.x), ref = t == -INFINITY ? 0.0f : t;
+            const float keep = exp2_fast(top - ref), w = exp2_fast(ml.x - ref);
+            top = t;
+            sum = __fmaf_rn(sum, keep, w * ml.y);
+            acc[0] = __fmaf_rn(acc[0], keep, w * v.x);
+            acc[1] = __fmaf_rn(acc[1], keep, w * v.y);
+            acc[2] = __fmaf_rn(acc[2], keep, w * v.z);
+            acc[3] = __fmaf_rn(acc[3], keep, w * v.w);
+        }
+        s_acc[threadIdx.x] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        if (threadIdx.x % kJoinCols == 0) s_ml[slice] = make_float2(top, sum);
+        __syncthreads();
+        if (slice) return;
+        const int n = min(SLICES, span.y - span.x + 1);
+        for (int i = 1; i < n; ++i) top = fmaxf(top, s_ml[i].x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        sum = acc[0] = acc[1] = acc[2] = acc[3] = 0.0f;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            const float2 ml = s_ml[i];
+            const float4 v = s_acc[i * kJoinCols + threadIdx.x];
+            const float w = exp2_fast(ml.x - ref);
+            sum = __fmaf_rn(w, ml.y, sum);
+            acc[0] = __fmaf_rn(w, v.x, acc[0]);
+            acc[1] = __fmaf_rn(w, v.y, acc[1]);
+            acc[2] = __fmaf_rn(w, v.z, acc[2]);
+            acc[3] = __fmaf_rn(w, v.w, acc[3]);
+        }
+        finish_row<BF>(a, (int64_t)b * a.Hq + h * a.group + rb * block_rows + r, c, acc, top, sum);
+        return;
+    }
+    // weights: 2^(v - lse) over the query heads of the KV head
+    int x = blockIdx.x - f.joins;
+    const int b = x / (f.mass_x * a.Hkv);
+    x -= b * f.mass_x * a.Hkv;
+    const int h = x / f.mass_x, t0 = (x - h * f.mass_x) * kThreads * kMassTokens, len = __ldg(a.lens + b);
+    if (len > a.max_len || t0 >= len) return;
+    const int first = a.window > 0 && len > a.window ? len - a.window : 0;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t at = (int64_t)b * a.Hkv + h;
+    const float *v = a.logits + at * a.max_len * a.group;
+    float w[kMassTokens], before[kMassTokens];                // added once, at the end: one rounding at the size of the mass
+    int t[kMassTokens];
+#pragma unroll
+    for (int j = 0; j < kMassTokens; ++j) {
+        t[j] = t0 + j * kThreads + threadIdx.x;
+        w[j] = 0.0f;
+        before[j] = a.mass_in && t[j] < len ? a.mass_in[at * a.mass_stride + t[j]] : 0.0f;
+    }
+    for (int g0 = 0; g0 < a.group; g0 += 64) {
+        const int n_g = min(64, a.group - g0);
+        for (int g = warp; g < n_g; g += kThreads / 32) {
+            const int rb = (g0 + g) / block_rows, r = g0 + g - rb * block_rows;
+            const int2 span = a.span[b * per_seq + h * a.blocks + rb];
+            float lse;
+            if (span.x < 0) {
+                lse = a.row_lse[at * a.group + g0 + g];
+            } else {                                          // the joining blocks run at the same time: again from the pieces
+                float top = -INFINITY, sum = 0.0f;
+                const float *from = a.part + (int64_t)r * pitch + f.cols;
+#pragma unroll 4
+                for (int i = span.x + lane; i <= span.y; i += 32) {
+                    const float2 ml = __ldcg(reinterpret_cast<const float2 *>(from + ((int64_t)i * 2 + (i == span.x)) * stride));
+                    lse_add(top, sum, ml.x, ml.y);
+                }
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const float m2 = __shfl_xor_sync(0xffffffffu, top, d), l2 = __shfl_xor_sync(0xffffffffu, sum, d);
+                    lse_add(top, sum, m2, l2);
+                }
+                lse = sum == 0.0f ? -INFINITY : top + log2f(sum);
+            }
+            if (lane == 0) s_lse[g] = lse;
+        }
+        __syncthreads();
+        for (int g = 0; g < n_g; ++g) {
+            const float lse = s_lse[g];
+            if (lse == -INFINITY) continue;                   // weights of 0
+#pragma unroll
+            for (int j = 0; j < kMassTokens; ++j)
+                if (t[j] < len && t[j] >= first) w[j] += exp2_fast(__ldcg(v + (int64_t)t[j] * a.group + g0 + g) - lse);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < kMassTokens; ++j)
+        if (t[j] < len) a.mass_out[at * a.mass_stride + t[j]] = before[j] + w[j];
+}
+
+template <bool BF>
+static int launch_finish(const DecodeArgs &a, FinishArgs f, cudaStream_t st)
+{
+    // few items: a block per item and part of its row, the slices as many as its pieces call for; more items than runs: a block
+    // per run, whose open item has pieces in few other runs
+    const int n_items = a.n_seqs * a.Hkv * a.blocks, slices = a.runs >= 32 * n_items ? 64 : (a.runs >= 4 * n_items ? 16 : 4);
+    f.by_item = n_items <= a.runs;
+    f.join_y = a.rows * (f.cols / 4) / kJoinCols;
+    f.joins = std::min(n_items, a.runs) * f.join_y;
+    const int tokens = slices * kJoinCols * kMassTokens;
+    f.mass_x = (a.max_len + tokens - 1) / tokens;
+    const dim3 grid(f.joins + (a.mass_out ? f.mass_x * a.Hkv * a.n_seqs : 0)), block(slices * kJoinCols);
+    LLMS_CUDA_TRY(launch_dependent(slices == 64 ? finish_kernel<BF, 64> : (slices == 16 ? finish_kernel<BF, 16> : finish_kernel<BF, 4>),
+                                   grid, block, 0, st, a, f));
+    return LLMS_OK;
+}
+
+constexpr int kRounds = 4, kRunTiles = 24, kMinTiles = 2;
 struct DecodeLayout {
-    int blocks_of_64, nt, rows, blocks;
-    uint64_t off_lse, off_plan, off_part, off_logits, total;
+    int blocks_of_64, mode, rows, blocks;
+    int runs;
+    uint64_t off_lse, off_span, off_open, off_part, off_logits, total;
 };
 
 static DecodeLayout decode_layout(const llms_kv_desc &d, int n_seqs, int max_len, bool with_mass)
@@ -674,56 +757,65 @@ static DecodeLayout decode_layout(const llms_kv_desc &d, int n_seqs, int max_len
     DecodeLayout t;
     const int group = d.n_q_heads / d.n_kv_heads;
     t.blocks_of_64 = (d.head_dim + 63) / 64;
-    t.nt = group > 8 ? 2 : 1;
-    t.rows = std::min(group, 8 * t.nt);
-    t.blocks = (group + 8 * t.nt - 1) / (8 * t.nt);
+    t.mode = group <= 4 ? 0 : (group <= 8 ? 1 : 2);
+    t.rows = std::min(group, t.mode == 2 ? 16 : 8);
+    t.blocks = (group + 15) / 16;
     t.off_lse = 0;
-    t.off_plan = round_up((uint64_t)n_seqs * d.n_q_heads * 4, 256);
-    t.off_part = t.off_plan + round_up((uint64_t)(n_seqs + 1) * 4, 256);
-    t.off_logits = t.off_part + round_up((uint64_t)sm_count() * 2 * t.rows * (t.blocks_of_64 * 64 + 2) * 4, 256);
+    // Runs: as many as the GPU has room for warps, or a small multiple of that where a run then still has kRunTiles tiles: the
+    // warps that get done early take the next ones.  The batch may turn out shorter than max_len says: working_runs
+    const uint64_t most_tiles = (uint64_t)n_seqs * d.n_kv_heads * t.blocks * (((uint64_t)max_len + kTile - 1) / kTile);
+    const uint64_t room = (uint64_t)sm_count() * (t.blocks_of_64 == 1 ? 10 : (t.blocks_of_64 == 2 ? 8 : (t.blocks_of_64 == 3 ? 5 : 4)));
+    const uint64_t rounds = std::min<uint64_t>(kRounds, std::max<uint64_t>(1, most_tiles / (room * kRunTiles)));
+    t.runs = (int)std::max<uint64_t>(1, std::min<uint64_t>(room * rounds, (most_tiles + kMinTiles - 1) / kMinTiles));
+    t.off_span = round_up((uint64_t)n_seqs * d.n_q_heads * 4, 256);
+    t.off_open = t.off_span + round_up((uint64_t)n_seqs * d.n_kv_heads * t.blocks * 8, 256);
+    t.off_part = t.off_open + round_up((uint64_t)t.runs * 4, 256);
+    t.off_logits = t.off_part + round_up((uint64_t)t.runs * 2 * t.rows * (t.blocks_of_64 * 64 + 4) * 4, 256);
     t.total = t.off_logits + (with_mass ? round_up((uint64_t)n_seqs * d.n_q_heads * (uint64_t)max_len * 4, 256) : 0);
     return t;
 }
 
-// A layer's K or V half as (channel, token, KV head), boxes of 64 channels x `piece` tokens; channels past head_dim read as 0
-static bool encode_half(CUtensorMap *map, const void *base, bool bf16, const llms_kv_desc &d, int piece)
+// A layer as (channel, token, block of 64 channels, KV head, K or V), boxes of 64 channels x `piece` tokens.  Where head_dim is a
+// multiple of 64 a box has all blocks, of K and of V: one copy per piece.  Elsewhere the channels stay one dimension, so
+// that those past head_dim read as 0, and a box has 64 of them.
+static bool encode_layer(CUtensorMap *map, const void *base, bool bf16, const llms_kv_desc &d, int piece, bool whole)
 {
-    const cuuint64_t dims[3] = {(cuuint64_t)d.head_dim, (cuuint64_t)d.n_tokens, (cuuint64_t)d.n_kv_heads};
     const cuuint64_t head = d.n_kv_heads == 1 ? (cuuint64_t)d.n_tokens * d.head_dim : (cuuint64_t)d.stride_h;
-    const cuuint64_t strides[2] = {(cuuint64_t)d.head_dim * 2, head * 2};
-    const cuuint32_t box[3] = {64, (cuuint32_t)piece, 1}, elem[3] = {1, 1, 1};
-    return tensor_map_encoder()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base),
+    const cuuint32_t n_blocks = whole ? d.head_dim / 64 : 1;
+    const cuuint64_t dims[5] = {whole ? 64 : (cuuint64_t)d.head_dim, (cuuint64_t)d.n_tokens, n_blocks, (cuuint64_t)d.n_kv_heads, 2};
+    const cuuint64_t strides[4] = {(cuuint64_t)d.head_dim * 2, 128, head * 2, (cuuint64_t)d.stride_s * 2};
+    const cuuint32_t box[5] = {64, (cuuint32_t)piece, n_blocks, 1, whole ? 2u : 1u}, elem[5] = {1, 1, 1, 1, 1};
+    return tensor_map_encoder()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, const_cast<void *>(base),
                                 dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool BF, int DB, int NT>
-static int launch_decode(DecodeArgs &a, const CUtensorMap &map_k, const CUtensorMap &map_v, cudaStream_t st)
+template <bool BF, int DB, int MODE>
+static int launch_decode(DecodeArgs &a, const CUtensorMap &map, cudaStream_t st)
 {
     using S = DecodeShape<DB>;
-    const size_t fixed = 1024 + S::kWarps * (piece_floats<DB>(a.rows) * 4 + sizeof(WarpSlots)) + round_up((uint64_t)(a.n_seqs + 1) * 4, 16);
-    const size_t most = 226 * 1024;
-    a.stages = (int)std::min<size_t>(kMaxStages, (most - fixed) / (S::kWarps * S::kStage));
-    a.min_tiles = S::kWarps;
-    const size_t smem = fixed + (size_t)S::kWarps * a.stages * S::kStage;
-    LLMS_CUDA_TRY(cudaFuncSetAttribute(decode_kernel<BF, DB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    decode_kernel<BF, DB, NT><<<a.ctas, S::kWarps * 32, smem, st>>>(a, map_k, map_v);
-    LLMS_CUDA_TRY(cudaGetLastError());
+    const size_t smem = 1024 + (size_t)S::kStages * S::kStage + (size_t)kQuerySlots * a.q_bytes;
+    LLMS_CUDA_TRY(cudaFuncSetAttribute(decode_kernel<BF, DB, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    LLMS_CUDA_TRY(launch_dependent(decode_kernel<BF, DB, MODE>, dim3(a.runs), dim3(32), smem, st, a, map));
     return LLMS_OK;
 }
 
 template <bool BF>
-static int launch_decode_shape(DecodeArgs &a, int db, int nt, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
+static int launch_decode_shape(DecodeArgs &a, int db, int mode, const CUtensorMap &map, cudaStream_t st)
 {
-    switch (db * 2 + nt - 1) {
-    case 2: return launch_decode<BF, 1, 1>(a, mk, mv, st);
-    case 3: return launch_decode<BF, 1, 2>(a, mk, mv, st);
-    case 4: return launch_decode<BF, 2, 1>(a, mk, mv, st);
-    case 5: return launch_decode<BF, 2, 2>(a, mk, mv, st);
-    case 6: return launch_decode<BF, 3, 1>(a, mk, mv, st);
-    case 7: return launch_decode<BF, 3, 2>(a, mk, mv, st);
-    case 8: return launch_decode<BF, 4, 1>(a, mk, mv, st);
-    case 9: return launch_decode<BF, 4, 2>(a, mk, mv, st);
+    switch (db * 3 + mode) {
+    case 3: return launch_decode<BF, 1, 0>(a, map, st);
+    case 4: return launch_decode<BF, 1, 1>(a, map, st);
+    case 5: return launch_decode<BF, 1, 2>(a, map, st);
+    case 6: return launch_decode<BF, 2, 0>(a, map, st);
+    case 7: return launch_decode<BF, 2, 1>(a, map, st);
+    case 8: return launch_decode<BF, 2, 2>(a, map, st);
+    case 9: return launch_decode<BF, 3, 0>(a, map, st);
+    case 10: return launch_decode<BF, 3, 1>(a, map, st);
+    case 11: return launch_decode<BF, 3, 2>(a, map, st);
+    case 12: return launch_decode<BF, 4, 0>(a, map, st);
+    case 13: return launch_decode<BF, 4, 1>(a, map, st);
+    case 14: return launch_decode<BF, 4, 2>(a, map, st);
     default: return LLMS_ERR_UNSUPPORTED;
     }
 }
@@ -776,7 +868,7 @@ extern "C" int llms_decode_attention(const llms_kv_desc *desc, int dtype, int la
     a.lse = lse;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     a.row_lse = reinterpret_cast<float *>(ws + lay.off_lse);
-    a.plan = reinterpret_cast<int32_t *>(ws + lay.off_plan);
+    a.span = reinterpret_cast<int2 *>(ws + lay.off_span);
     a.part = reinterpret_cast<float *>(ws + lay.off_part);
     a.logits = mass_out ? reinterpret_cast<float *>(ws + lay.off_logits) : nullptr;
     a.mass_in = mass_in; a.mass_out = mass_out;
@@ -788,16 +880,20 @@ extern "C" int llms_decode_attention(const llms_kv_desc *desc, int dtype, int la
     a.piece = 1;
     while (a.piece < kTile && a.chunk_len % (a.piece * 2) == 0) a.piece *= 2;
     a.scale_log2 = scale * kLog2e;
-    a.ctas = sm_count();
+    a.runs = lay.runs;
+    a.min_tiles = kMinTiles;
+    a.q_bytes = a.rows * a.d * 2;
+    a.open = reinterpret_cast<int32_t *>(ws + lay.off_open);
     const bool bf16 = dtype == LLMS_BF16;
-    CUtensorMap map_k, map_v;
-    if (!encode_half(&map_k, a.k, bf16, *desc, a.piece) || !encode_half(&map_v, a.v, bf16, *desc, a.piece)) return LLMS_ERR_UNSUPPORTED;
+    CUtensorMap map;
+    // a box may not hold more than one piece of a tile if K and V, or the blocks, are to lie a whole tile apart
+    a.whole_tile = a.d % 64 == 0 && a.piece == kTile;
+    if (!encode_layer(&map, a.k, bf16, *desc, a.piece, a.whole_tile)) return LLMS_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    rc = bf16 ? launch_decode_shape<true>(a, lay.blocks_of_64, lay.nt, map_k, map_v, st)
-              : launch_decode_shape<false>(a, lay.blocks_of_64, lay.nt, map_k, map_v, st);
+    rc = bf16 ? launch_decode_shape<true>(a, lay.blocks_of_64, lay.mode, map, st)
+              : launch_decode_shape<false>(a, lay.blocks_of_64, lay.mode, map, st);
     if (rc) return rc;
-    const dim3 join_grid(a.ctas, a.rows);
-    LLMS_CUDA_TRY(launch_dependent(bf16 ? join_kernel<true> : join_kernel<false>, join_grid, dim3(kJoinThreads), 0, st, a, lay.blocks_of_64 * 64));
-    if (mass_out) LLMS_CUDA_TRY(launch_dependent(mass_kernel, dim3((max_len + 255) / 256, a.Hkv, n_seqs), dim3(256), 0, st, a));
-    return LLMS_OK;
+    FinishArgs f{};
+    f.cols = lay.blocks_of_64 * 64;
+    return bf16 ? launch_finish<true>(a, f, st) : launch_finish<false>(a, f, st);
 }
