@@ -1,8 +1,32 @@
-// Token eviction by accumulated attention weight: per (layer, sequence, KV head) the heaviest tokens are selected, then
-// their K and V rows are closed up.
+// Token eviction by accumulated attention weight: per (layer, sequence, KV head) the heaviest tokens stay, and their K and V
+// rows and masses are closed up.
+//
+// Selection (select_kernel, one CTA per (layer, sequence, KV head)).  The masses' order as unsigned keys (mass_key); the key of the
+// quota-th heaviest candidate is found digit by digit, 11, 11 and 10 bits, counting keys per digit value in shared memory; keys
+// above it stay, and of those equal to it the first ones.  A last pass in the order of positions numbers the kept tokens.  The
+// first digit has sign, exponent and two bits of the fraction, so that masses that differ by powers of two - attention
+// weights do - spread over the counters.  The masses stay in shared memory for the passes if they fit.
+//
+// Rows (move_kernel).  A kept row is read and written once, 8 * head_dim bytes for K and V together: memory-bound, in pieces of a row
+// (2 * head_dim bytes) at scattered places.  Whole rows are moved by neighbouring lanes, rows in the order of their
+// positions by neighbouring warps, so that the memory sees its pages' accesses together.  To other slots every CTA takes a
+// range of rows.  In place a kept row's new position never lies behind its old one: a CTA that goes up in batches, each read
+// completely before it is written, never overwrites a row that it has yet to read.  Where there are few slabs a cluster
+// shares one, batch by batch.
+#include <algorithm>
+
+#include <cooperative_groups.h>
+
 #include "llms_internal.cuh"
 
 namespace llms {
+
+namespace cg = cooperative_groups;
+
+constexpr int kSliceTokens = 16384;               // masses a CTA holds in shared memory; of longer sequences it reads them again
+constexpr int kBins = 2048;
+constexpr int kMoveThreads = 256, kInFlight = 4;  // 16-byte vectors a thread has in flight
+constexpr int kMaxCluster = 8;
 
 struct EvictArgs {
     const float *mass;
@@ -12,128 +36,254 @@ struct EvictArgs {
     int32_t *kept, *new_lens;
     int64_t stride_l, stride_s, stride_h, mass_stride;
     int table_stride, dst_stride, n_seqs, max_len, L, Hkv, d, chunk_len, n_slots, budget, recent;
+    int in_smem;                                  // the masses of a sequence fit into shared memory
+    int parts, batches;                           // move: CTAs per slab; batches of rows a CTA takes (0: all, in place)
 };
 
-constexpr int kSelectThreads = 1024;
-
-// Order of the masses as an unsigned key: larger mass, larger key; NaN and -inf are both 0 and lie below every other
-// value, -0 equals +0.
-__device__ __forceinline__ uint32_t mass_key(float m)
+// Order of the masses as an unsigned key: larger mass, larger key; NaN and -inf are the same and lie below every other value,
+// -0 equals +0.  No key is above 0xff800000 (+inf) or below 0x007fffff.  odd: the sequence may have such values.
+__device__ __forceinline__ uint32_t mass_key(float m, bool odd)
 {
-    if (isnan(m) || m == -INFINITY) return 0u;
-    const uint32_t u = m == 0.0f ? 0u : __float_as_uint(m);
-    return (u >> 31) ? ~u : (u | 0x80000000u);
+    const uint32_t u = __float_as_uint(m);
+    uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    if (odd) {
+        if (k == 0x7fffffffu) k = 0x80000000u;
+        if ((u << 1) > 0xff000000u) k = 0x007fffffu;
+    }
+    return k;
+}
+__device__ __forceinline__ bool is_odd(float m)
+{
+    const uint32_t u = __float_as_uint(m);
+    return u == 0x80000000u || (u << 1) > 0xff000000u;
 }
 
-// Select: one CTA per (KV head, sequence, layer).  The key of the quota-th heaviest candidate is found digit by digit
-// (four passes of 256 bins), then one pass in the order of positions numbers the kept tokens.
-__global__ void __launch_bounds__(kSelectThreads) select_kernel(const EvictArgs a)
+__device__ __forceinline__ int slot_row(const int32_t *row, int chunk_len, int n_slots, int t)
 {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t warp_gt[32], warp_eq[32];
-    __shared__ uint32_t s_prefix, s_need;
-    const int h = blockIdx.x, b = blockIdx.y, l = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int len = a.lens[b];
+    const int chunk = t / chunk_len, slot = __ldg(row + chunk);
+    return (unsigned)slot < (unsigned)n_slots ? slot * chunk_len + (t - chunk * chunk_len) : -1;
+}
+
+__global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
+{
+    __shared__ __align__(16) uint32_t hist[kBins];
+    __shared__ uint32_t warp_sum[32], warp_eq[32], s_digit, s_need;
+    extern __shared__ float slice[];
+    const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = threads >> 5;
+    int x = blockIdx.x;
+    const int h = x % a.Hkv;
+    x /= a.Hkv;
+    const int b = x % a.n_seqs, l = x / a.n_seqs;
     const int64_t row = ((int64_t)l * a.n_seqs + b) * a.Hkv + h;
     const float *mass = a.mass + row * a.mass_stride;
     float *mass_out = a.mass_out + row * a.mass_stride;
     int32_t *kept = a.kept + row * a.budget;
+    uint4 *hist4 = reinterpret_cast<uint4 *>(hist);
+    for (int i = tid; i < kBins / 4; i += threads) hist4[i] = make_uint4(0, 0, 0, 0);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int len = __ldg(a.lens + b);
     const bool bad = len < 0 || len > a.max_len;
-    const int n = bad ? 0 : len, m = min(a.budget, n), recent = min(a.recent, m);
-    const int cand = n - recent, quota = m - recent;
-    uint32_t limit = 0, need = quota;             // keys above `limit` stay, and the first `need` ones equal to it
-    if (quota > 0 && quota < cand) {
-        uint32_t prefix = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = threadIdx.x; i < 256; i += kSelectThreads) hist[i] = 0;
+    const int n = bad ? 0 : len, m = min(a.budget, n), recent = min(a.recent, m), cand = n - recent, quota = m - recent;
+    // Keys above `limit` stay, and the first `need` ones equal to it.  Nothing to rank: all candidates, or none
+    const bool ranked = quota > 0 && quota < cand;
+    uint32_t limit = quota == 0 ? 0xffffffffu : 0u, need = ranked ? quota : 0;
+    const float *from = a.in_smem ? slice : mass;
+    __syncthreads();                              // hist is cleared
+    bool odd = false;
+#pragma unroll 4
+    for (int i = tid; i < n; i += threads) {
+        const float w = __ldcg(mass + i);
+        if (a.in_smem) slice[i] = w;
+        odd |= is_odd(w);
+        if (ranked && i < cand) atomicAdd(&hist[mass_key(w, true) >> 21], 1u);
+    }
+    odd = __syncthreads_or(odd);
+    if (ranked) {
+#pragma unroll 1
+        for (int shift = 21; ; shift = max(0, shift - 11)) {
+            // from the highest value down: thread t has 2048 / threads neighbouring ones
+            const int each = kBins / threads, top = kBins - 1 - tid * each;
+            uint32_t sum = 0;
+            if (each >= 4)
+                for (int i = 0; i < each / 4; ++i) {
+                    const uint4 x = hist4[top / 4 - i];
+                    sum += x.x + x.y + x.z + x.w;
+                }
+            else
+                for (int i = 0; i < each; ++i) sum += hist[top - i];
+            uint32_t upto = sum;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const uint32_t up = __shfl_up_sync(0xffffffffu, upto, d);
+                if (lane >= d) upto += up;
+            }
+            if (lane == 31) warp_sum[warp] = upto;
             __syncthreads();
-            const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-            for (int t = threadIdx.x; t < cand; t += kSelectThreads) {
-                const uint32_t k = mass_key(mass[t]);
-                if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+            uint32_t before = lane < warp ? warp_sum[lane] : 0u;
+            before = __reduce_add_sync(0xffffffffu, before);
+            upto += before;
+            uint32_t above = upto - sum;          // keys with higher values
+            if (above < need && upto >= need) {
+                int i = 0;
+                while (above + hist[top - i] < need) above += hist[top - i++];
+                s_digit = top - i;
+                s_need = need - above;
             }
             __syncthreads();
-            if (threadIdx.x == 0) {
-                int bin = 255;
-                while (bin > 0 && hist[bin] < need) need -= hist[bin--];
-                s_prefix = prefix | ((uint32_t)bin << shift);
-                s_need = need;
-            }
-            __syncthreads();
-            prefix = s_prefix;
+            limit |= s_digit << shift;
             need = s_need;
-        }
-        limit = prefix;
-    }
-    uint32_t gt_base = 0, eq_base = 0;
-    for (int t0 = 0; t0 < n; t0 += kSelectThreads) {
-        const int t = t0 + threadIdx.x;
-        float w = 0.0f;
-        bool gt = false, eq = false;
-        if (t < n) {
-            w = mass[t];
-            const uint32_t k = mass_key(w);
-            gt = t >= cand || (quota > 0 && k > limit) || quota >= cand;
-            eq = !gt && quota > 0 && k == limit;
-        }
-        const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
-        if (lane == 0) {
-            warp_gt[warp] = __popc(bg);
-            warp_eq[warp] = __popc(be);
-        }
-        __syncthreads();                          // also: every mass of this tile has been read
-        uint32_t gt_before = gt_base + __popc(bg & ((1u << lane) - 1)), eq_before = eq_base + __popc(be & ((1u << lane) - 1));
-        for (int w2 = 0; w2 < 32; ++w2) {
-            const uint32_t g = warp_gt[w2], e = warp_eq[w2];
-            if (w2 < warp) {
-                gt_before += g;
-                eq_before += e;
+            if (shift == 0) break;
+            for (int i = tid; i < kBins / 4; i += threads) hist4[i] = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+            const int next = max(0, shift - 11), bits = shift - next;          // 11, then 10
+            const uint32_t want = limit >> shift;
+#pragma unroll 8
+            for (int i = tid; i < cand; i += threads) {
+                const uint32_t k = mass_key(from[i], odd);
+                if (k >> shift == want) atomicAdd(&hist[(k >> next) & ((1u << bits) - 1u)], 1u);
             }
-            gt_base += g;
-            eq_base += e;
+            __syncthreads();
         }
-        if (gt || (eq && eq_before < need)) {
-            const uint32_t j = gt_before + min(eq_before, need);
-            kept[j] = t;
-            mass_out[j] = w;
+    }
+    const bool everything = quota >= cand;
+    auto stays = [&](int t, float w, bool &gt, bool &eq) {
+        const uint32_t k = mass_key(w, odd);
+        gt = t >= cand || everything || k > limit;
+        eq = !gt && need > 0 && k == limit;
+    };
+    const uint32_t below = (1u << lane) - 1u;
+    if (a.in_smem) {
+        // a warp takes neighbouring tokens, 32 at a time: it counts its ones, then numbers them in the order of positions
+        const int share = ((n + n_warps - 1) / n_warps + 31) & ~31, w0 = min(n, warp * share), w1 = min(n, w0 + share);
+        uint32_t g = 0, e = 0;
+#pragma unroll 4
+        for (int t = w0 + lane; t < w1; t += 32) {
+            bool gt, eq;
+            stays(t, slice[t], gt, eq);
+            g += gt;
+            e += eq;
+        }
+        g = __reduce_add_sync(0xffffffffu, g);
+        e = __reduce_add_sync(0xffffffffu, e);
+        if (lane == 0) {
+            warp_sum[warp] = g;
+            warp_eq[warp] = e;
+        }
+        __syncthreads();
+        g = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane] : 0u);
+        e = __reduce_add_sync(0xffffffffu, lane < warp ? warp_eq[lane] : 0u);
+#pragma unroll 2
+        for (int t0 = w0; t0 < w1; t0 += 32) {
+            const int t = t0 + lane;
+            bool gt = false, eq = false;
+            const float w = t < w1 ? slice[t] : 0.0f;
+            if (t < w1) stays(t, w, gt, eq);
+            const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
+            const uint32_t e_me = e + __popc(be & below), to = g + __popc(bg & below) + min(e_me, need);
+            if (gt || (eq && e_me < need)) {
+                kept[to] = t;
+                mass_out[to] = w;
+            }
+            g += __popc(bg);
+            e += __popc(be);
+        }
+    } else {
+        // a token per thread, tile by tile: what is written lies at or before the tokens that have been read, so mass_out may be
+        // the same array
+        uint32_t g = 0, e = 0;
+#pragma unroll 1
+        for (int t0 = 0; t0 < n; t0 += threads) {
+            const int t = t0 + tid;
+            bool gt = false, eq = false;
+            float w = 0.0f;
+            if (t < n) {
+                w = mass[t];
+                stays(t, w, gt, eq);
+            }
+            const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
+            __syncthreads();                      // the sums of the tile before have been read
+            if (lane == 0) {
+                warp_sum[warp] = __popc(bg);
+                warp_eq[warp] = __popc(be);
+            }
+            __syncthreads();
+            const uint32_t wg = lane < n_warps ? warp_sum[lane] : 0u, we = lane < n_warps ? warp_eq[lane] : 0u;
+            const uint32_t e_me = e + __reduce_add_sync(0xffffffffu, lane < warp ? we : 0u) + __popc(be & below);
+            const uint32_t to = g + __reduce_add_sync(0xffffffffu, lane < warp ? wg : 0u) + __popc(bg & below) + min(e_me, need);
+            if (gt || (eq && e_me < need)) {
+                kept[to] = t;
+                mass_out[to] = w;
+            }
+            g += __reduce_add_sync(0xffffffffu, wg);
+            e += __reduce_add_sync(0xffffffffu, we);
         }
         __syncthreads();
     }
-    for (int j = m + threadIdx.x; j < a.budget; j += kSelectThreads) kept[j] = -1;
-    for (int t = m + threadIdx.x; t < n; t += kSelectThreads) mass_out[t] = 0.0f;
-    if (threadIdx.x == 0 && l == 0 && h == 0) a.new_lens[b] = bad ? -1 : m;
+    for (int j = m + tid; j < a.budget; j += threads) kept[j] = -1;
+    for (int t = m + tid; t < n; t += threads) mass_out[t] = 0.0f;
+    if (tid == 0 && l == 0 && h == 0) a.new_lens[b] = bad ? -1 : m;
 }
 
-__device__ __forceinline__ int64_t slot_row(const int32_t *row, int chunk_len, int n_slots, int t)
+// A slab (K or V of a KV head) of one sequence; its CTAs take batches of rows in turn.
+template <bool IN_PLACE, bool CLUSTER>
+__global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a)
 {
-    const int slot = __ldg(row + t / chunk_len);
-    return (unsigned)slot < (unsigned)n_slots ? (int64_t)slot * chunk_len + t % chunk_len : -1;
-}
-
-// Move: one CTA per (K or V of a KV head, sequence, layer).  A kept row's new position never lies behind its old one, so
-// going up in tiles of rows, each read completely before it is written, is safe in place.
-__global__ void __launch_bounds__(256) move_kernel(const EvictArgs a)
-{
-    const int h = blockIdx.x >> 1, s = blockIdx.x & 1, b = blockIdx.y, l = blockIdx.z;
+    constexpr int kMostRows = kMoveThreads / 2 * kInFlight;                   // of a batch: rows have at least two vectors
+    __shared__ int2 rows[2][kMostRows];           // old and new row, of this round and the next; a new row of -1: nothing to move
+    const int vec = a.d / 8, at_once = kMoveThreads / vec, batch = at_once * kInFlight, tid = threadIdx.x;
+    const int r = tid / vec, c = tid - r * vec;
+    const bool live = r < at_once;
+    const int part = blockIdx.x % a.parts;
+    int x = blockIdx.x / a.parts;
+    const int half = x & 1;
+    x >>= 1;
+    const int h = x % a.Hkv;
+    x /= a.Hkv;
+    const int b = x % a.n_seqs, l = x / a.n_seqs;
     const int32_t *kept = a.kept + (((int64_t)l * a.n_seqs + b) * a.Hkv + h) * a.budget;
-    uint4 *base = reinterpret_cast<uint4 *>(a.kv + l * a.stride_l + s * a.stride_s + h * a.stride_h);
-    const int vec = a.d / 8;
-    const int m = a.new_lens[b];
-    const int32_t *src_tab = a.table + (int64_t)b * a.table_stride;
-    const int32_t *dst_tab = a.dst_table ? a.dst_table + (int64_t)b * a.dst_stride : src_tab;
-    const int rows_at_once = 256 / vec;
-    const int r = threadIdx.x / vec, c = threadIdx.x % vec;
-    for (int j0 = 0; j0 < m; j0 += rows_at_once) {
-        const int j = j0 + r;
-        uint4 v;
-        int64_t src = -1, dst = -1;
-        if (r < rows_at_once && j < m) {
-            src = slot_row(src_tab, a.chunk_len, a.n_slots, kept[j]);
-            dst = slot_row(dst_tab, a.chunk_len, a.n_slots, j);
-            if (src >= 0) v = base[src * vec + c];
+    const int32_t *from = a.table + (int64_t)b * a.table_stride;
+    const int32_t *to = IN_PLACE ? from : a.dst_table + (int64_t)b * a.dst_stride;
+    uint4 *slab = reinterpret_cast<uint4 *>(a.kv + l * a.stride_l + half * a.stride_s + h * a.stride_h) + c;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int n = __ldg(a.lens + b);
+    if (n < 0 || n > a.max_len) return;
+    const int m = min(a.budget, n);
+    if (IN_PLACE && m == n) return;               // every row stays where it is
+    const int first = IN_PLACE ? part * batch : part * a.batches * batch, step = IN_PLACE ? a.parts * batch : batch;
+    const int rounds = IN_PLACE ? (m + step - 1) / step : min(a.batches, (m - first + batch - 1) / batch);
+    auto look_up = [&](int k) {
+        const int j0 = first + k * step;
+        for (int i = tid; i < batch; i += kMoveThreads) {
+            const int j = j0 + i;
+            int2 x = make_int2(-1, -1);
+            if (j < m) {
+                x.x = slot_row(from, a.chunk_len, a.n_slots, __ldcg(kept + j));
+                x.y = slot_row(to, a.chunk_len, a.n_slots, j);
+                if (x.x < 0 || x.x == x.y) x.y = -1;
+            }
+            rows[k & 1][i] = x;
         }
-        __syncthreads();
-        if (src >= 0 && dst >= 0 && src != dst) base[dst * vec + c] = v;
+    };
+    if (rounds > 0) look_up(0);
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < rounds; ++k) {            // in a cluster every CTA goes through every round
+        uint4 v[kInFlight];
+        int d[kInFlight];
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u) {
+            const int2 x = live ? rows[k & 1][u * at_once + r] : make_int2(-1, -1);
+            d[u] = x.y;
+            if (x.y >= 0) v[u] = __ldcg(slab + (int64_t)x.x * vec);
+        }
+        if (k + 1 < rounds) look_up(k + 1);       // while the vectors are on their way
+        if constexpr (CLUSTER) cg::this_cluster().sync();
+        else __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u)
+            if (d[u] >= 0) slab[(int64_t)d[u] * vec] = v[u];
     }
 }
 
@@ -158,7 +308,8 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     if (!aligned(mass, 4) || !aligned(mass_out, 4) || !aligned(chunk_table, 4) || !aligned(lens, 4) || !aligned(dst_table, 4) ||
         !aligned(kept, 4) || !aligned(new_lens, 4))
         return LLMS_ERR_MISALIGNED;
-    if (desc->n_layers > 65535) return LLMS_ERR_UNSUPPORTED;
+    const int64_t items = (int64_t)desc->n_layers * n_seqs * desc->n_kv_heads;
+    if (items > 0x7fffffff / 64) return LLMS_ERR_UNSUPPORTED;
     EvictArgs a{};
     a.mass = mass; a.mass_out = mass_out;
     a.kv = static_cast<uint16_t *>(kv);
@@ -170,9 +321,39 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     a.chunk_len = desc->chunk_len; a.n_slots = n_chunks(*desc);
     a.budget = budget; a.recent = recent;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    select_kernel<<<dim3(a.Hkv, n_seqs, a.L), kSelectThreads, 0, st>>>(a);
-    LLMS_CUDA_TRY(cudaGetLastError());
-    move_kernel<<<dim3(a.Hkv * 2, n_seqs, a.L), 256, 0, st>>>(a);
-    LLMS_CUDA_TRY(cudaGetLastError());
+    // a thread of the selection has 32 masses, if that makes no more than 1024 threads
+    int threads = 128;
+    while (threads < 1024 && threads * 32 < max_len) threads *= 2;
+    a.in_smem = max_len <= kSliceTokens;
+    const size_t smem = a.in_smem ? round_up((uint64_t)max_len * 4, 16) : 0;
+    LLMS_CUDA_TRY(cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    LLMS_CUDA_TRY(launch_dependent(select_kernel, dim3((unsigned)items), dim3(threads), smem, st, a));
+
+    constexpr int kFillCtas = 592;
+    const int batch = kMoveThreads / (a.d / 8) * kInFlight, most_batches = (most + batch - 1) / batch;
+    void (*kernel)(EvictArgs);
+    if (dst_table) {
+        a.batches = 8;
+        a.parts = (most_batches + a.batches - 1) / a.batches;
+        kernel = move_kernel<false, false>;
+    } else {
+        a.parts = 1;
+        while (a.parts < kMaxCluster && items * 2 * a.parts < kFillCtas && a.parts < most_batches) a.parts *= 2;
+        kernel = a.parts > 1 ? move_kernel<true, true> : move_kernel<true, false>;
+    }
+    if (items * 2 * a.parts > 0x7fffffff) return LLMS_ERR_UNSUPPORTED;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(items * 2 * a.parts));
+    cfg.blockDim = dim3(kMoveThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = a.parts;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = !dst_table && a.parts > 1 ? 2 : 1;
+    LLMS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
     return LLMS_OK;
 }
