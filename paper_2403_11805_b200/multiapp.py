@@ -14,6 +14,7 @@ import torch
 
 from . import binding as B
 from . import synth
+from .serving import Serving
 
 
 class MultiApp:
@@ -36,6 +37,7 @@ class MultiApp:
         self.table["ctx_id"] = np.repeat(np.arange(self.n_ctx), self.cpc)
         self.table["chunk_id"] = np.tile(np.arange(self.cpc), self.n_ctx)
         self.slot = np.full(n, -1, dtype=np.int64)
+        self.lengths = [shape.n_tokens] * self.n_ctx   # tokens per context; chunks behind them hold nothing (Serving.shrink)
         self.free = list(range(n_slots - 1, -1, -1))
         self.checksum = np.zeros(n, dtype=np.uint32)
         self.clean = np.zeros(n, dtype=bool)      # the record in the arena matches what sits in the slot
@@ -242,11 +244,42 @@ class MultiApp:
         if bad:
             raise RuntimeError(f"{bad} records failed their checksum on the way in")
 
+    # ------------------------------------------------------------------ contexts that change their length while served
+    def rows(self, c):
+        """Rows of the chunk table that hold tokens of context c."""
+        return np.arange(c * self.cpc, c * self.cpc + -(-self.lengths[c] // self.shape.chunk_len))
+
+    def take_slots(self, n):
+        """n free slots; chunks of unlocked contexts are reclaimed in LCTRU order if there are not enough."""
+        need = n - len(self.free)
+        if need > 0:
+            order = B.lctru_order(self.table)
+            if self.orders is not None:
+                self.orders.append((self.table.copy(), order.copy()))
+            if len(order) < need:
+                raise RuntimeError("pool too small for the locked working sets")
+            self._evict(order[:need])
+        return [self.free.pop() for _ in range(n)]
+
+    def occupy(self, row, slot):
+        """A chunk that a served context grew into: resident, locked, not in the arena."""
+        self.slot[row] = slot
+        self.table["resident"][row], self.table["locked"][row] = 1, 1
+        self.table["last_access_step"][row] = self.step_no
+        self.clean[row] = False
+
+    def vacate(self, rows):
+        """Chunks that hold no token any more: their slots are free, nothing of them is kept."""
+        for r in rows:
+            self.free.append(int(self.slot[r]))
+        self.slot[rows] = -1
+        self.table["resident"][rows], self.table["locked"][rows] = 0, 0
+        self.clean[rows] = False
+
     # ------------------------------------------------------------------ one step of the trace
     def draw_contexts(self, k):
         """k distinct contexts that are not fully resident, uniformly (splitmix64 stream of the seed)."""
-        resident = self.table["resident"].reshape(self.n_ctx, self.cpc).all(axis=1)
-        cand = [c for c in range(self.n_ctx) if not resident[c]]
+        cand = [c for c in range(self.n_ctx) if not self.table["resident"][self.rows(c)].all()]
         picks = []
         while len(picks) < k and cand:
             z = synth.splitmix64_int((synth.stream_key(self.seed, 7) + self._draw * 0x9E3779B97F4A7C15) & ((1 << 64) - 1))
@@ -254,17 +287,18 @@ class MultiApp:
             picks.append(cand.pop(z % len(cand)))
         return picks
 
-    def step(self, k=8):
-        """Serve k contexts: lock, evict in LCTRU order as far as needed, load, touch, unlock."""
+    def step(self, k=8, serve=None):
+        """Serve k contexts: lock, evict in LCTRU order as far as needed, load, touch, unlock.  serve: called with a Serving
+        of the contexts while their working sets are resident and locked."""
         self.step_no += 1
         if not hasattr(self, "_ev_t0"):
             self._ev_t0, self._ev_ready = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         self._ev_t0.record(self.main)
         ctxs = self.draw_contexts(k)
-        locked_rows = np.concatenate([np.arange(c * self.cpc, (c + 1) * self.cpc) for c in ctxs])
+        locked_rows = np.concatenate([self.rows(c) for c in ctxs])
         self.table["locked"][locked_rows] = 1            # working-set lock
         for c in ctxs:
-            rows = np.arange(c * self.cpc, (c + 1) * self.cpc)
+            rows = self.rows(c)
             missing = rows[self.table["resident"][rows] == 0]
             need = len(missing) - len(self.free)
             if need > 0:
@@ -278,6 +312,11 @@ class MultiApp:
                 self._load(missing)
             self.table["last_access_step"][rows] = self.step_no
         self._ev_ready.record(self.main)                 # the working sets are resident: inference could start
+        if serve is not None:
+            batch = Serving(self, ctxs)
+            serve(batch)
+            batch.close()
+            locked_rows = np.concatenate([self.rows(c) for c in ctxs])
         self.clean[locked_rows] = False                  # a served context counts as modified by its call
         self.table["locked"][locked_rows] = 0
         self._end_of_step()                              # also settles the write-back left running by the step before
@@ -294,9 +333,9 @@ class MultiApp:
         return ctxs
 
     def context_kv(self, c):
-        """The resident KV of context c gathered from its slots: fp16 [L, 2, H, T, d] (device)."""
+        """The resident KV of context c gathered from its slots, whole chunks: fp16 [L, 2, H, T, d] (device)."""
         sh = self.shape
-        rows = np.arange(c * self.cpc, (c + 1) * self.cpc)
+        rows = self.rows(c)
         assert (self.slot[rows] >= 0).all()
         CL = sh.chunk_len
         parts = [self.pool[..., int(s) * CL:(int(s) + 1) * CL, :] for s in self.slot[rows]]

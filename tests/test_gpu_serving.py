@@ -1,0 +1,123 @@
+"""Contexts of the multi-app pool served token by token: decode, shrink, growth into new chunks, and Reclaim / Load of what is left."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2403_11805_b200 import synth
+from paper_2403_11805_b200.multiapp import MultiApp
+from gpu_helpers import bits_view, odesc
+from paged_reference import Batch, attend, bits, evict
+
+pytestmark = pytest.mark.gpu
+
+
+def batch_of(s, sh, app):
+    """The served batch as the reference sees it."""
+    bt = Batch([1] * len(s.ctxs), heads=sh.n_kv_heads, group=sh.n_q_heads // sh.n_kv_heads, dim=sh.head_dim, chunk=sh.chunk_len,
+               layers=sh.n_layers, max_len=s.capacity, junk=0.0)
+    bt.lens, bt.table, bt.n_slots, bt.kv, bt.mass = s.lengths.tolist(), s.table.cpu(), app.n_slots, app.pool.cpu(), s.mass.cpu()
+    assert s.lens.tolist() == bt.lens and np.array_equal(bt.table.numpy(), s.host_table)
+    return bt
+
+
+def consistent(app):
+    res = app.slot >= 0
+    assert np.array_equal(res, app.table["resident"] != 0)
+    assert sorted(app.slot[res].tolist() + app.free) == list(range(app.n_slots))
+    live = np.concatenate([app.rows(c) for c in range(app.n_ctx)])
+    assert set(np.flatnonzero(res)) <= set(live.tolist())
+
+
+@pytest.mark.parametrize("aot", [False, True], ids=["reclaim", "aot"])
+def test_decode_shrink_and_swap(aot):
+    sh = synth.KVShape("apps", 2, 2, 8, 64, 128, 16, 64, window=4, seed=5, n_contexts=6)      # 8 chunks per context
+    app = MultiApp(sh, n_slots=19, seed=2, log_ops=True, aot=aot)
+    app.build()
+    g = torch.Generator().manual_seed(1)
+    state = {}
+
+    def serve(s):
+        n = len(s.ctxs)
+
+        def token():
+            s.advance()
+            for layer in range(sh.n_layers):
+                bt = batch_of(s, sh, app)
+                bt.qkv = torch.randn(n, sh.n_q_heads + 2 * sh.n_kv_heads, sh.head_dim, generator=g).half()
+                q, k, v = bt.qkv.split([sh.n_q_heads, sh.n_kv_heads, sh.n_kv_heads], dim=1)
+                bt.q, bt.k_new, bt.v_new = q, k, v
+                dev = bt.qkv.cuda().split([sh.n_q_heads, sh.n_kv_heads, sh.n_kv_heads], dim=1)
+                out = s.decode(layer, *dev)
+                want, _, wmass, wkv, (ot, _, mt) = attend(bt, layer, append=True, mass_in=bt.mass[layer], mass_before=bt.mass[layer])
+                assert ((out.cpu().double() - want).abs() <= ot).all()
+                assert ((s.mass[layer].cpu().double() - wmass).abs() <= mt).all()
+                assert torch.equal(bits(app.pool.cpu()), bits(wkv))
+
+        if (s.lengths == s.capacity).any():
+            with pytest.raises(RuntimeError):
+                s.advance()
+            s.shrink(100, 100)                                # nothing accumulated yet: the last 100 tokens
+        for _ in range(5):
+            token()
+        bt = batch_of(s, sh, app)
+        kept = s.shrink(70, 9)
+        want = evict(bt, bt.mass, 70, 9, None, bt.mass)
+        assert torch.equal(kept.cpu(), want[0]) and torch.equal(s.mass.cpu(), want[2]) and torch.equal(bits(app.pool.cpu()), bits(want[3]))
+        assert s.lens.tolist() == [70] * n
+        consistent(app)
+        for _ in range(12):                                   # 70 -> 82 tokens: into a sixth chunk
+            token()
+        assert s.lens.tolist() == [82] * n
+        for i, c in enumerate(s.ctxs):
+            assert (s.host_table[i] >= 0).sum() == 6
+        state["served"] = {c: app.pool.cpu()[..., bt_rows, :] for c, bt_rows in zip(s.ctxs, [batch_of(s, sh, app).rows(i, upto=96) for i in range(n)])}
+
+    first = app.step(k=2, serve=serve)
+    consistent(app)
+    assert [app.lengths[c] for c in first] == [82, 82]
+    saved = dict(state["served"])
+    back = set()
+    for _ in range(12):                                       # others push them out; they come back as their records say
+        consistent(app)
+        before = len(app.ops)
+        for c in app.step(k=1):
+            loaded = {row for op, row, _ in app.ops[before:] if op == "load"}
+            if c in saved and c not in back:
+                back.add(c)
+                got = app.context_kv(c).cpu()
+                one = odesc(sh.with_(n_tokens=sh.chunk_len))
+                for i in range(6):
+                    chunk = np.ascontiguousarray(bits_view(saved[c])[..., i * 16:(i + 1) * 16, :])
+                    if c * app.cpc + i not in loaded:         # stayed in its slot
+                        assert np.array_equal(bits_view(got[..., i * 16:(i + 1) * 16, :]), chunk), (c, i)
+                        continue
+                    buf, meta = oracle.compress_chunks(one, chunk, [0], [int(app.table["bits"][c * app.cpc + i])])
+                    out = np.zeros_like(chunk)
+                    oracle.decompress_chunks(one, buf, meta, out)
+                    assert np.array_equal(bits_view(got[..., i * 16:(i + 1) * 16, :]), out), (c, i)
+    app.finish()
+    consistent(app)
+    assert back, "no served context came back within the steps"
+
+
+def test_serving_keeps_to_its_capacity():
+    sh = synth.KVShape("apps", 1, 2, 2, 64, 64, 16, 64, window=4, seed=1, n_contexts=4)
+    app = MultiApp(sh, n_slots=8, seed=3)
+    app.build()
+
+    def serve(s):
+        with pytest.raises(RuntimeError):
+            s.advance()
+        assert s.lengths.tolist() == [64, 64] and s.lens.tolist() == [64, 64]
+        s.shrink(64, 4)                                       # nothing to drop
+        assert s.lens.tolist() == [64, 64] and (s.host_table >= 0).all()
+        s.shrink(1, 1)
+        assert s.lens.tolist() == [1, 1] and (s.host_table >= 0).sum() == 2
+
+    served = app.step(k=2, serve=serve)
+    consistent(app)
+    assert [app.lengths[c] for c in served] == [1, 1]
+    for _ in range(4):
+        app.step(k=2)
+        consistent(app)
