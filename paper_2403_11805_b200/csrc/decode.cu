@@ -57,9 +57,10 @@ struct DecodeArgs {
     int64_t q_stride, new_stride, stride_h, mass_stride;
     int table_stride, n_seqs, max_len, window, Hkv, Hq, group, d, chunk_len, n_slots;
     int blocks;                                   // blocks of query rows per KV head
-    int piece;                                    // tokens per TMA box: the largest power of two up to 16 that divides chunk_len
-    int rows, runs;                               // query rows kept per partial result, runs at most (CTAs of the main kernel)
-    int min_tiles;                                // a run has at least this many tiles (but for the last tiles of a small batch)
+    int piece_shift;                              // log2 of the tokens per TMA box: the largest power of two up to 16 that divides chunk_len
+    Divisor by_chunk, by_blocks, by_per_seq, by_mass_x, by_hkv;
+    int rows;                                     // query rows kept per partial result
+    int runs, grid_runs, few_tiles;               // runs; runs at most (CTAs of the main kernel), which up to few_tiles tiles are cut into
     int q_bytes;                                  // of an item's query rows
     int whole_tile;                               // one TMA copy takes K and V of a tile
     float scale_log2;
@@ -79,10 +80,23 @@ __device__ __forceinline__ SeqTiles seq_tiles(const DecodeArgs &a, int len)
     return s;
 }
 
-// Runs that the batch's tiles are cut into, and which tiles are whose
-__device__ __forceinline__ int working_runs(const DecodeArgs &a, int total) { return min(a.runs, max(1, total / a.min_tiles)); }
-__device__ __forceinline__ int run_begin(int total, int runs, int i) { return (int)((int64_t)total * i / runs); }
-__device__ __forceinline__ int run_of(int total, int runs, int tile) { return (int)((((int64_t)tile + 1) * runs - 1) / total); }
+// The runs that the batch's tiles are cut into: the first `longer` ones have a tile more than the others.
+constexpr int kMinTiles = 2;                      // tiles that a run has at least (but for the last ones of a small batch)
+struct Runs {
+    int n, tiles, longer;
+    __device__ __forceinline__ Runs(const DecodeArgs &a, int total)
+    {
+        n = max(1, min(total <= a.few_tiles ? a.grid_runs : a.runs, total / kMinTiles));
+        tiles = (int)((unsigned)total / (unsigned)n);
+        longer = total - n * tiles;
+    }
+    __device__ __forceinline__ int begin(int i) const { return i * tiles + min(i, longer); }
+    __device__ __forceinline__ int of(int tile) const                         // the run that has a tile
+    {
+        const int border = longer * (tiles + 1);
+        return tile < border ? (int)((unsigned)tile / (unsigned)(tiles + 1)) : longer + (int)((unsigned)(tile - border) / (unsigned)max(tiles, 1));
+    }
+};
 
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, int c4, unsigned long long *bar)
 {
@@ -214,8 +228,8 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
         if (lane >= d) incl += up;
     }
     const int total = __shfl_sync(0xffffffffu, incl, 31);
-    const int runs = working_runs(a, total);
-    const int w0 = run < runs ? run_begin(total, runs, run) : 0, w1 = run < runs ? run_begin(total, runs, run + 1) : 0;
+    const Runs runs(a, total);
+    const int w0 = run < runs.n ? runs.begin(run) : 0, w1 = run < runs.n ? runs.begin(run + 1) : 0;
     int open_item = -1;                                       // the item that begins in this run and goes on behind it
 
     if (w0 < w1) {
@@ -233,23 +247,23 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
         SeqTiles c_s = f_s;
 
         // ---- feeding: lane i looks up piece i % n_pieces of the tile i / n_pieces behind `base`
-        const int n_pieces = kTile / a.piece, ahead = a.piece * 2;            // pieces per tile, tiles per look-up
+        const int n_shift = 4 - a.piece_shift, n_pieces = 1 << n_shift, ahead = 32 >> n_shift;   // pieces per tile, tiles per look-up
         int f_row, f_slot, f_q;                                               // row in its chunk, slot, sequence
         bool f_need;
         uint32_t f_h, f_qb;                                                   // KV head (and first query row << 16); bytes of query rows,
                                                                               // which come with the first tile of an item
         auto look_up = [&](int base) {
-            const int idx = base + lane / n_pieces, last = min(base + ahead, w1) - 1;
+            const int idx = base + (lane >> n_shift), last = min(base + ahead, w1) - 1;
             f_need = false;
             f_slot = -1;
             f_qb = 0;
             for (;;) {
                 if (idx >= f_base && idx <= last && idx < f_base + f_s.n * per_seq) {
                     const int hb = (idx - f_base) / f_s.n, tile = idx - f_base - hb * f_s.n;
-                    const int tok = (f_s.tile0 + tile) * kTile + (lane & (n_pieces - 1)) * a.piece;
-                    f_need = tok < f_s.len && tok + a.piece > f_s.first;
-                    f_h = hb / a.blocks;
-                    const int chunk = tok / a.chunk_len;
+                    const int tok = (f_s.tile0 + tile) * kTile + ((lane & (n_pieces - 1)) << a.piece_shift);
+                    f_need = tok < f_s.len && tok + (1 << a.piece_shift) > f_s.first;
+                    f_h = a.by_blocks(hb);
+                    const int chunk = a.by_chunk(tok);
                     f_row = tok - chunk * a.chunk_len;
                     if (f_need) f_slot = __ldg(a.table + (int64_t)f_seq * a.table_stride + chunk);
                     if ((idx == w0 || tile == 0) && (lane & (n_pieces - 1)) == 0) {
@@ -274,18 +288,18 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
                 q_mask = __ballot_sync(0xffffffffu, f_qb != 0);
                 fetched = true;
             }
-            const int lead = (issued - base) * n_pieces;
+            const int lead = (issued - base) << n_shift;
             const bool with_q = q_mask >> lead & 1;
             if (with_q && q_issued - q_read >= kQuerySlots) return;           // its query rows have no place yet
             const uint32_t mine = ((1u << n_pieces) - 1u) << lead;
             unsigned long long *bar = &full[stage_in];
             poisoned = (poisoned & ~(1u << stage_in)) | (bad_mask & mine ? 1u << stage_in : 0u);
-            if (lane == lead) mbar_expect_tx(bar, __popc(ok_mask & mine) * a.piece * 128 * DB * 2 + f_qb);
+            if (lane == lead) mbar_expect_tx(bar, (__popc(ok_mask & mine) << a.piece_shift) * 128 * DB * 2 + f_qb);
             __syncwarp();
             if (mine >> lane & 1) {
                 if (ok_mask >> lane & 1) {
                     const int row = f_slot * a.chunk_len + f_row, h = f_h & 0xffff;
-                    const uint32_t dst = ring_addr + stage_in * S::kStage + (lane - lead) * a.piece * 128;
+                    const uint32_t dst = ring_addr + stage_in * S::kStage + ((lane - lead) << a.piece_shift) * 128;
                     if (a.whole_tile) {
                         tma_load_5d(dst, &map, 0, row, 0, h, 0, bar);
                     } else {
@@ -322,7 +336,7 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
 
 #pragma unroll 1
         for (int idx = w0; idx < w1;) {                       // the items that this run has tiles of
-            const int h = c_hb / a.blocks, rb = c_hb - h * a.blocks;
+            const int h = a.by_blocks(c_hb), rb = c_hb - h * a.blocks;
             const int row0 = rb * 8 * NT, have = min(a.rows, a.group - row0);     // query rows of this item
             const int tile_end = min(c_s.n, c_tile + w1 - idx);
             const bool item_ends = tile_end == c_s.n;
@@ -337,7 +351,7 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
                     const uint16_t *from = c < half ? a.k_new : a.v_new;
                     if (c < 2 * half) fresh[i] = __ldg(reinterpret_cast<const uint4 *>(from + c_seq * a.new_stride + (int64_t)h * a.d) + (c < half ? c : c - half));
                 }
-                fresh_slot = __ldg(a.table + (int64_t)c_seq * a.table_stride + (c_s.len - 1) / a.chunk_len);
+                fresh_slot = __ldg(a.table + (int64_t)c_seq * a.table_stride + a.by_chunk(c_s.len - 1));
             }
             bool good = mbar_wait(&full[stage], phase, &gave_up);
             // query rows as the MMA's second operand; columns beyond the item's rows repeat others (nobody reads their
@@ -392,7 +406,7 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
                     if (append && tile + 1 == c_s.n) {
                         const int t = c_s.len - 1, r = t - tok0;
                         const bool inside = (unsigned)fresh_slot < (unsigned)a.n_slots && rb == 0;
-                        const int64_t to = (int64_t)h * a.stride_h + ((int64_t)fresh_slot * a.chunk_len + t % a.chunk_len) * a.d;
+                        const int64_t to = (int64_t)h * a.stride_h + ((int64_t)fresh_slot * a.chunk_len + (t - a.by_chunk(t) * a.chunk_len)) * a.d;
 #pragma unroll
                         for (int i = 0; i < (DB <= 2 ? 1 : 2); ++i) {
                             const int half = a.d / 8, cv = lane + i * 32, c = cv < half ? cv : cv - half;
@@ -566,7 +580,7 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
             const int item = c_seq * per_seq + c_hb;
             if (tile_begin == 0) {                            // the item begins here: say who has its tiles
                 if (!item_ends) open_item = item;
-                if (lane == 0) a.span[item] = item_ends ? make_int2(-1, 0) : make_int2(run, run_of(total, runs, item_begin + c_s.n - 1));
+                if (lane == 0) a.span[item] = item_ends ? make_int2(-1, 0) : make_int2(run, runs.of(item_begin + c_s.n - 1));
             }
             if (idx < w1) {
                 c_tile = 0;
@@ -597,7 +611,7 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
 // Items that span runs are joined, block (x, y) taking kJoinCols groups of four channels of the y-th part of item x (by_item) or of
 // the item that is open at the end of run x, in SLICES over the runs that have pieces of it.  The other blocks: the weights
 // of kMassTokens tokens per thread.
-constexpr int kJoinCols = 16, kMassTokens = 4;
+constexpr int kJoinCols = 16, kMassTokens = 2;
 struct FinishArgs {
     int by_item, joins, join_y, cols, mass_x;
 };
@@ -624,7 +638,7 @@ __global__ void __launch_bounds__(SLICES * kJoinCols) finish_kernel(const Decode
         const int x = blockIdx.x / f.join_y, y = blockIdx.x - x * f.join_y;
         const int item = f.by_item ? x : a.open[x];
         if (item < 0) return;
-        const int b = item / per_seq, hb = item - b * per_seq, h = hb / a.blocks, rb = hb - h * a.blocks;
+        const int b = a.by_per_seq(item), hb = item - b * per_seq, h = a.by_blocks(hb), rb = hb - h * a.blocks;
         const int2 span = a.span[item];
         if (f.by_item && seq_tiles(a, __ldg(a.lens + b)).n == 0) return;   // its span was never written
         if (span.x < 0) return;
@@ -671,22 +685,23 @@ __global__ void __launch_bounds__(SLICES * kJoinCols) finish_kernel(const Decode
         return;
     }
     // weights: 2^(v - lse) over the query heads of the KV head
-    int x = blockIdx.x - f.joins;
-    const int b = x / (f.mass_x * a.Hkv);
-    x -= b * f.mass_x * a.Hkv;
-    const int h = x / f.mass_x, t0 = (x - h * f.mass_x) * kThreads * kMassTokens, len = __ldg(a.lens + b);
+    const int x = blockIdx.x - f.joins;
+    const int bh = a.by_mass_x(x), b = a.by_hkv(bh), h = bh - b * a.Hkv, t0 = (x - bh * f.mass_x) * kThreads * kMassTokens, len = __ldg(a.lens + b);
     if (len > a.max_len || t0 >= len) return;
     const int first = a.window > 0 && len > a.window ? len - a.window : 0;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t at = (int64_t)b * a.Hkv + h;
     const float *v = a.logits + at * a.max_len * a.group;
     float w[kMassTokens], before[kMassTokens];                // added once, at the end: one rounding at the size of the mass
+    float4 early[kMassTokens];                                // the logits, where a token has four: asked for before the log-sums
     int t[kMassTokens];
+    const bool four = a.group == 4;
 #pragma unroll
     for (int j = 0; j < kMassTokens; ++j) {
         t[j] = t0 + j * kThreads + threadIdx.x;
         w[j] = 0.0f;
         before[j] = a.mass_in && t[j] < len ? a.mass_in[at * a.mass_stride + t[j]] : 0.0f;
+        if (four && t[j] < len && t[j] >= first) early[j] = __ldcg(reinterpret_cast<const float4 *>(v) + t[j]);
     }
     for (int g0 = 0; g0 < a.group; g0 += 64) {
         const int n_g = min(64, a.group - g0);
@@ -714,12 +729,17 @@ __global__ void __launch_bounds__(SLICES * kJoinCols) finish_kernel(const Decode
             if (lane == 0) s_lse[g] = lse;
         }
         __syncthreads();
-        for (int g = 0; g < n_g; ++g) {
-            const float lse = s_lse[g];
-            if (lse == -INFINITY) continue;                   // weights of 0
+        auto weight = [&](float x, float lse) { return lse == -INFINITY ? 0.0f : exp2_fast(x - lse); };
+        if (four) {
 #pragma unroll
             for (int j = 0; j < kMassTokens; ++j)
-                if (t[j] < len && t[j] >= first) w[j] += exp2_fast(__ldcg(v + (int64_t)t[j] * a.group + g0 + g) - lse);
+                if (t[j] < len && t[j] >= first)
+                    w[j] = (weight(early[j].x, s_lse[0]) + weight(early[j].y, s_lse[1])) + (weight(early[j].z, s_lse[2]) + weight(early[j].w, s_lse[3]));
+        } else {
+            for (int g = 0; g < n_g; ++g)
+#pragma unroll
+                for (int j = 0; j < kMassTokens; ++j)
+                    if (t[j] < len && t[j] >= first) w[j] += weight(__ldcg(v + (int64_t)t[j] * a.group + g0 + g), s_lse[g]);
         }
         __syncthreads();
     }
@@ -729,26 +749,28 @@ __global__ void __launch_bounds__(SLICES * kJoinCols) finish_kernel(const Decode
 }
 
 template <bool BF>
-static int launch_finish(const DecodeArgs &a, FinishArgs f, cudaStream_t st)
+static int launch_finish(DecodeArgs &a, FinishArgs f, cudaStream_t st)
 {
     // few items: a block per item and part of its row, the slices as many as its pieces call for; more items than runs: a block
     // per run, whose open item has pieces in few other runs
-    const int n_items = a.n_seqs * a.Hkv * a.blocks, slices = a.runs >= 32 * n_items ? 64 : (a.runs >= 4 * n_items ? 16 : 4);
-    f.by_item = n_items <= a.runs;
+    const int n_items = a.n_seqs * a.Hkv * a.blocks, slices = a.grid_runs >= 128 * n_items ? 64 : (a.grid_runs >= 16 * n_items ? 16 : 4);
+    f.by_item = n_items <= a.grid_runs;
     f.join_y = a.rows * (f.cols / 4) / kJoinCols;
-    f.joins = std::min(n_items, a.runs) * f.join_y;
+    f.joins = std::min(n_items, a.grid_runs) * f.join_y;
     const int tokens = slices * kJoinCols * kMassTokens;
     f.mass_x = (a.max_len + tokens - 1) / tokens;
+    a.by_mass_x = Divisor(f.mass_x);
     const dim3 grid(f.joins + (a.mass_out ? f.mass_x * a.Hkv * a.n_seqs : 0)), block(slices * kJoinCols);
     LLMS_CUDA_TRY(launch_dependent(slices == 64 ? finish_kernel<BF, 64> : (slices == 16 ? finish_kernel<BF, 16> : finish_kernel<BF, 4>),
                                    grid, block, 0, st, a, f));
     return LLMS_OK;
 }
 
-constexpr int kRounds = 4, kRunTiles = 24, kMinTiles = 2;
+constexpr int kRounds = 4, kRunTiles = 16;
+constexpr int kRoom[4] = {8, 5, 4, 3};           // warps per SM, by blocks of 64 channels
 struct DecodeLayout {
     int blocks_of_64, mode, rows, blocks;
-    int runs;
+    int runs, grid_runs, few_tiles;
     uint64_t off_lse, off_span, off_open, off_part, off_logits, total;
 };
 
@@ -761,16 +783,22 @@ static DecodeLayout decode_layout(const llms_kv_desc &d, int n_seqs, int max_len
     t.rows = std::min(group, t.mode == 2 ? 16 : 8);
     t.blocks = (group + 15) / 16;
     t.off_lse = 0;
-    // Runs: as many as the GPU has room for warps, or a small multiple of that where a run then still has kRunTiles tiles: the
-    // warps that get done early take the next ones.  The batch may turn out shorter than max_len says: working_runs
+    // Runs: one for each of the warps that it takes to keep the memory busy (with more tiles on their way at once the memory gets
+    // slower), or a small multiple of that where a run then still has kRunTiles tiles: the warps that get done early take
+    // the next ones.  A batch of many items whose tiles come to less than six a run is cut finer (few items: their many
+    // pieces would cost more in finish_kernel).  max_len is a bound; the device knows better (struct Runs)
     const uint64_t most_tiles = (uint64_t)n_seqs * d.n_kv_heads * t.blocks * (((uint64_t)max_len + kTile - 1) / kTile);
-    const uint64_t room = (uint64_t)sm_count() * (t.blocks_of_64 == 1 ? 10 : (t.blocks_of_64 == 2 ? 8 : (t.blocks_of_64 == 3 ? 5 : 4)));
+    const uint64_t room = (uint64_t)sm_count() * kRoom[t.blocks_of_64 - 1];
     const uint64_t rounds = std::min<uint64_t>(kRounds, std::max<uint64_t>(1, most_tiles / (room * kRunTiles)));
-    t.runs = (int)std::max<uint64_t>(1, std::min<uint64_t>(room * rounds, (most_tiles + kMinTiles - 1) / kMinTiles));
+    const uint64_t finest = std::max<uint64_t>(1, most_tiles / kMinTiles);
+    t.few_tiles = (int)(6 * room);
+    t.runs = (int)std::min<uint64_t>(room * rounds, finest);
+    const bool many_items = (uint64_t)n_seqs * d.n_kv_heads * t.blocks * 4 >= room;
+    t.grid_runs = many_items ? (int)std::max<uint64_t>(t.runs, std::min<uint64_t>(2 * room, finest)) : t.runs;
     t.off_span = round_up((uint64_t)n_seqs * d.n_q_heads * 4, 256);
     t.off_open = t.off_span + round_up((uint64_t)n_seqs * d.n_kv_heads * t.blocks * 8, 256);
-    t.off_part = t.off_open + round_up((uint64_t)t.runs * 4, 256);
-    t.off_logits = t.off_part + round_up((uint64_t)t.runs * 2 * t.rows * (t.blocks_of_64 * 64 + 4) * 4, 256);
+    t.off_part = t.off_open + round_up((uint64_t)t.grid_runs * 4, 256);
+    t.off_logits = t.off_part + round_up((uint64_t)t.grid_runs * 2 * t.rows * (t.blocks_of_64 * 64 + 4) * 4, 256);
     t.total = t.off_logits + (with_mass ? round_up((uint64_t)n_seqs * d.n_q_heads * (uint64_t)max_len * 4, 256) : 0);
     return t;
 }
@@ -796,7 +824,7 @@ static int launch_decode(DecodeArgs &a, const CUtensorMap &map, cudaStream_t st)
     using S = DecodeShape<DB>;
     const size_t smem = 1024 + (size_t)S::kStages * S::kStage + (size_t)kQuerySlots * a.q_bytes;
     LLMS_CUDA_TRY(cudaFuncSetAttribute(decode_kernel<BF, DB, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    LLMS_CUDA_TRY(launch_dependent(decode_kernel<BF, DB, MODE>, dim3(a.runs), dim3(32), smem, st, a, map));
+    LLMS_CUDA_TRY(launch_dependent(decode_kernel<BF, DB, MODE>, dim3(a.grid_runs), dim3(32), smem, st, a, map));
     return LLMS_OK;
 }
 
@@ -877,18 +905,20 @@ extern "C" int llms_decode_attention(const llms_kv_desc *desc, int dtype, int la
     a.Hkv = desc->n_kv_heads; a.Hq = desc->n_q_heads; a.group = a.Hq / a.Hkv; a.d = desc->head_dim;
     a.chunk_len = desc->chunk_len; a.n_slots = n_chunks(*desc);
     a.blocks = lay.blocks; a.rows = lay.rows;
-    a.piece = 1;
-    while (a.piece < kTile && a.chunk_len % (a.piece * 2) == 0) a.piece *= 2;
+    while (a.piece_shift < 4 && a.chunk_len % (2 << a.piece_shift) == 0) ++a.piece_shift;
+    a.by_chunk = Divisor(a.chunk_len);
+    a.by_blocks = Divisor(a.blocks);
+    a.by_per_seq = Divisor(a.Hkv * a.blocks);
+    a.by_hkv = Divisor(a.Hkv);
     a.scale_log2 = scale * kLog2e;
-    a.runs = lay.runs;
-    a.min_tiles = kMinTiles;
+    a.runs = lay.runs; a.grid_runs = lay.grid_runs; a.few_tiles = lay.few_tiles;
     a.q_bytes = a.rows * a.d * 2;
     a.open = reinterpret_cast<int32_t *>(ws + lay.off_open);
     const bool bf16 = dtype == LLMS_BF16;
     CUtensorMap map;
     // a box may not hold more than one piece of a tile if K and V, or the blocks, are to lie a whole tile apart
-    a.whole_tile = a.d % 64 == 0 && a.piece == kTile;
-    if (!encode_layer(&map, a.k, bf16, *desc, a.piece, a.whole_tile)) return LLMS_ERR_UNSUPPORTED;
+    a.whole_tile = a.d % 64 == 0 && a.piece_shift == 4;
+    if (!encode_layer(&map, a.k, bf16, *desc, 1 << a.piece_shift, a.whole_tile)) return LLMS_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     rc = bf16 ? launch_decode_shape<true>(a, lay.blocks_of_64, lay.mode, map, st)
               : launch_decode_shape<false>(a, lay.blocks_of_64, lay.mode, map, st);

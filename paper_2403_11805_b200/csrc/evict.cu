@@ -1,11 +1,13 @@
 // Token eviction by accumulated attention weight: per (layer, sequence, KV head) the heaviest tokens stay, and their K and V
 // rows and masses are closed up.
 //
-// Selection (select_kernel, one CTA per (layer, sequence, KV head)).  The masses' order as unsigned keys (mass_key); the key of the
-// quota-th heaviest candidate is found digit by digit, 11, 11 and 10 bits, counting keys per digit value in shared memory; keys
-// above it stay, and of those equal to it the first ones.  A last pass in the order of positions numbers the kept tokens.  The
-// first digit has sign, exponent and two bits of the fraction, so that masses that differ by powers of two - attention
-// weights do - spread over the counters.  The masses stay in shared memory for the passes if they fit.
+// Selection (select_kernel, a CTA, or where there are few of them a cluster of CTAs, per (layer, sequence, KV head)).  The masses'
+// order as unsigned keys (mass_key); the key of the quota-th heaviest candidate is found digit by digit, 11, 11 and 10 bits,
+// counting keys per digit value in shared memory (added up over the cluster's shared memories); keys above it stay, and of
+// those equal to it the first ones.  A last pass in the order of positions numbers the kept tokens.  The first digit has
+// sign, exponent and two bits of the fraction, so that masses that differ by powers of two - attention weights do - spread
+// over the counters, and few are left with the limit's first digit: these are listed in the pass that counts the kept
+// tokens, and the other digits are found from the list.  The masses stay in shared memory for the passes if they fit.
 //
 // Rows (move_kernel).  A kept row is read and written once, 8 * head_dim bytes for K and V together: memory-bound, in pieces of a row
 // (2 * head_dim bytes) at scattered places.  Whole rows are moved by neighbouring lanes, rows in the order of their
@@ -23,7 +25,8 @@ namespace llms {
 
 namespace cg = cooperative_groups;
 
-constexpr int kSliceTokens = 16384;               // masses a CTA holds in shared memory; of longer sequences it reads them again
+constexpr int kSliceTokens = 16384;               // masses that a CTA holds in shared memory; of longer sequences it reads them again,
+constexpr int kSliceTokensShared = 49152;         // but a cluster's CTAs hold theirs
 constexpr int kBins = 2048;
 constexpr int kMoveThreads = 256, kInFlight = 4;  // 16-byte vectors a thread has in flight
 constexpr int kMaxCluster = 8;
@@ -36,7 +39,10 @@ struct EvictArgs {
     int32_t *kept, *new_lens;
     int64_t stride_l, stride_s, stride_h, mass_stride;
     int table_stride, dst_stride, n_seqs, max_len, L, Hkv, d, chunk_len, n_slots, budget, recent;
-    int in_smem;                                  // the masses of a sequence fit into shared memory
+    int list_room;                                // keys with the limit's first digit that are listed
+    int in_smem, select_shift, warps_shift;       // the masses fit into shared memory; log2 of the CTAs per (layer, sequence, KV head)
+                                                  // and of the warps per CTA
+    Divisor by_chunk, by_parts, by_vec;
     int parts, batches;                           // move: CTAs per slab; batches of rows a CTA takes (0: all, in place)
 };
 
@@ -58,60 +64,81 @@ __device__ __forceinline__ bool is_odd(float m)
     return u == 0x80000000u || (u << 1) > 0xff000000u;
 }
 
-__device__ __forceinline__ int slot_row(const int32_t *row, int chunk_len, int n_slots, int t)
+__device__ __forceinline__ int slot_row(const EvictArgs &a, const int32_t *row, int t)
 {
-    const int chunk = t / chunk_len, slot = __ldg(row + chunk);
-    return (unsigned)slot < (unsigned)n_slots ? slot * chunk_len + (t - chunk * chunk_len) : -1;
+    const int chunk = a.by_chunk(t), slot = __ldg(row + chunk);
+    return (unsigned)slot < (unsigned)a.n_slots ? slot * a.chunk_len + (t - chunk * a.chunk_len) : -1;
 }
 
+template <bool CLUSTER>
 __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
 {
-    __shared__ __align__(16) uint32_t hist[kBins];
-    __shared__ uint32_t warp_sum[32], warp_eq[32], s_digit, s_need;
-    extern __shared__ float slice[];
+    // counters, one set per digit in a cluster (other CTAs may still read the last one) and one for the sums; list; masses
+    extern __shared__ uint4 smem_select[];
+    uint32_t *hist = reinterpret_cast<uint32_t *>(smem_select);
+    uint32_t *const sums = hist + (CLUSTER ? 3 * kBins : 0);
+    uint2 *list = reinterpret_cast<uint2 *>(sums + kBins);                     // key, token
+    float *slice = reinterpret_cast<float *>(list + a.list_room);
+    __shared__ uint32_t warp_sum[32], warp_eq[32], warp_add[2][32], s_digit, s_need, s_bin, s_listed, s_counts[2];
     const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = threads >> 5;
-    int x = blockIdx.x;
-    const int h = x % a.Hkv;
-    x /= a.Hkv;
-    const int b = x % a.n_seqs, l = x / a.n_seqs;
+    const int parts = CLUSTER ? 1 << a.select_shift : 1, part = CLUSTER ? blockIdx.x & (parts - 1) : 0;
+    const int h = CLUSTER ? blockIdx.x >> a.select_shift : blockIdx.x, b = blockIdx.y, l = blockIdx.z;
     const int64_t row = ((int64_t)l * a.n_seqs + b) * a.Hkv + h;
     const float *mass = a.mass + row * a.mass_stride;
     float *mass_out = a.mass_out + row * a.mass_stride;
     int32_t *kept = a.kept + row * a.budget;
-    uint4 *hist4 = reinterpret_cast<uint4 *>(hist);
-    for (int i = tid; i < kBins / 4; i += threads) hist4[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < (CLUSTER ? 3 : 1) * kBins / 4; i += threads) smem_select[i] = make_uint4(0, 0, 0, 0);
     grid_dependency_wait();
     grid_launch_dependents();
     const int len = __ldg(a.lens + b);
     const bool bad = len < 0 || len > a.max_len;
     const int n = bad ? 0 : len, m = min(a.budget, n), recent = min(a.recent, m), cand = n - recent, quota = m - recent;
+    // this CTA's tokens, from t0 on, and how many of them are candidates
+    const int share = CLUSTER ? (n + parts - 1) >> a.select_shift : n, t0 = CLUSTER ? min(n, part * share) : 0, count = min(n, t0 + share) - t0;
+    const int mine = max(0, min(count, cand - t0));
     // Keys above `limit` stay, and the first `need` ones equal to it.  Nothing to rank: all candidates, or none
     const bool ranked = quota > 0 && quota < cand;
     uint32_t limit = quota == 0 ? 0xffffffffu : 0u, need = ranked ? quota : 0;
     const float *from = a.in_smem ? slice : mass;
+    // a warp's own tokens, for the passes in the order of positions
+    const int warp_shift = a.warps_shift, each_warp = (((count + n_warps - 1) >> warp_shift) + 31) & ~31, w0 = min(count, warp * each_warp), w1 = min(count, w0 + each_warp);
+    uint32_t n_gt = 0, n_eq = 0;                  // of the warp's tokens: above the limit, equal to it
+    const uint32_t below = (1u << lane) - 1u;
+    if (tid == 0) s_listed = 0;
+    if (tid < 32) warp_add[0][tid] = warp_add[1][tid] = 0;
     __syncthreads();                              // hist is cleared
     bool odd = false;
 #pragma unroll 4
-    for (int i = tid; i < n; i += threads) {
-        const float w = __ldcg(mass + i);
+    for (int i = tid; i < count; i += threads) {
+        const float w = __ldcg(mass + t0 + i);
         if (a.in_smem) slice[i] = w;
         odd |= is_odd(w);
-        if (ranked && i < cand) atomicAdd(&hist[mass_key(w, true) >> 21], 1u);
+        if (ranked && i < mine) atomicAdd(&hist[mass_key(w, true) >> 21], 1u);
     }
     odd = __syncthreads_or(odd);
+    bool listed = false;
     if (ranked) {
 #pragma unroll 1
         for (int shift = 21; ; shift = max(0, shift - 11)) {
             // from the highest value down: thread t has 2048 / threads neighbouring ones
-            const int each = kBins / threads, top = kBins - 1 - tid * each;
+            const int each = kBins >> (5 + a.warps_shift), top = kBins - 1 - tid * each;
             uint32_t sum = 0;
-            if (each >= 4)
+            if constexpr (CLUSTER) {
+                cg::this_cluster().sync();
+                for (int i = 0; i < each; ++i) {
+                    uint32_t c = 0;
+                    for (int p = 0; p < parts; ++p) c += cg::this_cluster().map_shared_rank(hist, p)[top - i];
+                    sums[top - i] = c;
+                    sum += c;
+                }
+            } else if (each >= 4) {
                 for (int i = 0; i < each / 4; ++i) {
-                    const uint4 x = hist4[top / 4 - i];
+                    const uint4 x = smem_select[top / 4 - i];
                     sum += x.x + x.y + x.z + x.w;
                 }
-            else
+            } else {
                 for (int i = 0; i < each; ++i) sum += hist[top - i];
+            }
             uint32_t upto = sum;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -120,81 +147,133 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
             }
             if (lane == 31) warp_sum[warp] = upto;
             __syncthreads();
-            uint32_t before = lane < warp ? warp_sum[lane] : 0u;
-            before = __reduce_add_sync(0xffffffffu, before);
-            upto += before;
+            upto += __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane] : 0u);
             uint32_t above = upto - sum;          // keys with higher values
             if (above < need && upto >= need) {
                 int i = 0;
-                while (above + hist[top - i] < need) above += hist[top - i++];
+                while (above + sums[top - i] < need) above += sums[top - i++];
                 s_digit = top - i;
                 s_need = need - above;
+                s_bin = sums[top - i];
             }
             __syncthreads();
             limit |= s_digit << shift;
             need = s_need;
             if (shift == 0) break;
-            for (int i = tid; i < kBins / 4; i += threads) hist4[i] = make_uint4(0, 0, 0, 0);
-            __syncthreads();
-            const int next = max(0, shift - 11), bits = shift - next;          // 11, then 10
+            if constexpr (CLUSTER) {
+                hist += kBins;
+            } else {
+                for (int i = tid; i < kBins / 4; i += threads) smem_select[i] = make_uint4(0, 0, 0, 0);
+                __syncthreads();
+            }
             const uint32_t want = limit >> shift;
+            if (shift == 21) {
+                listed = s_bin <= (uint32_t)a.list_room;                       // the whole cluster's: the same for all its CTAs
+                if (listed) {
+#pragma unroll 2
+                    for (int i0 = w0; i0 < w1; i0 += 32) {
+                        const int i = i0 + lane;
+                        const uint32_t k = i < mine ? mass_key(from[i], odd) : 0u;
+                        n_gt += i < w1 && (i >= mine || k >> 21 > want);
+                        const uint32_t bl = __ballot_sync(0xffffffffu, i < mine && i < w1 && k >> 21 == want);
+                        if (bl) {
+                            uint32_t at = 0;
+                            if (lane == 0) at = atomicAdd(&s_listed, __popc(bl));
+                            at = __shfl_sync(0xffffffffu, at, 0) + __popc(bl & below);
+                            if (bl >> lane & 1) list[at] = make_uint2(k, i);
+                        }
+                    }
+                    __syncthreads();
+                }
+            }
+            const int next = max(0, shift - 11), bits = shift - next;          // 11, then 10
+            if (listed) {
+                for (int i = tid; i < (int)s_listed; i += threads) {
+                    const uint32_t k = list[i].x;
+                    if (k >> shift == want) atomicAdd(&hist[(k >> next) & ((1u << bits) - 1u)], 1u);
+                }
+            } else {
 #pragma unroll 8
-            for (int i = tid; i < cand; i += threads) {
-                const uint32_t k = mass_key(from[i], odd);
-                if (k >> shift == want) atomicAdd(&hist[(k >> next) & ((1u << bits) - 1u)], 1u);
+                for (int i = tid; i < mine; i += threads) {
+                    const uint32_t k = mass_key(from[i], odd);
+                    if (k >> shift == want) atomicAdd(&hist[(k >> next) & ((1u << bits) - 1u)], 1u);
+                }
             }
             __syncthreads();
         }
     }
     const bool everything = quota >= cand;
-    auto stays = [&](int t, float w, bool &gt, bool &eq) {
+    auto stays = [&](int i, float w, bool &gt, bool &eq) {                     // token t0 + i
         const uint32_t k = mass_key(w, odd);
-        gt = t >= cand || everything || k > limit;
+        gt = i >= mine || everything || k > limit;
         eq = !gt && need > 0 && k == limit;
     };
-    const uint32_t below = (1u << lane) - 1u;
-    if (a.in_smem) {
+    if (CLUSTER || a.in_smem || a.mass != a.mass_out) {
         // a warp takes neighbouring tokens, 32 at a time: it counts its ones, then numbers them in the order of positions
-        const int share = ((n + n_warps - 1) / n_warps + 31) & ~31, w0 = min(n, warp * share), w1 = min(n, w0 + share);
-        uint32_t g = 0, e = 0;
+        if (listed) {
+            for (int i = tid; i < (int)s_listed; i += threads) {
+                const uint2 x = list[i];
+                if (x.x >= limit) atomicAdd(&warp_add[x.x == limit][x.y / (uint32_t)each_warp], 1u);
+            }
+        } else {
 #pragma unroll 4
-        for (int t = w0 + lane; t < w1; t += 32) {
-            bool gt, eq;
-            stays(t, slice[t], gt, eq);
-            g += gt;
-            e += eq;
+            for (int i = w0 + lane; i < w1; i += 32) {
+                bool gt, eq;
+                stays(i, from[i], gt, eq);
+                n_gt += gt;
+                n_eq += eq;
+            }
         }
+        __syncthreads();
+        uint32_t g = n_gt, e = n_eq;
         g = __reduce_add_sync(0xffffffffu, g);
         e = __reduce_add_sync(0xffffffffu, e);
         if (lane == 0) {
-            warp_sum[warp] = g;
-            warp_eq[warp] = e;
+            warp_sum[warp] = g + warp_add[0][warp];
+            warp_eq[warp] = e + warp_add[1][warp];
         }
         __syncthreads();
-        g = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane] : 0u);
-        e = __reduce_add_sync(0xffffffffu, lane < warp ? warp_eq[lane] : 0u);
+        const uint32_t all_g = lane < n_warps ? warp_sum[lane] : 0u, all_e = lane < n_warps ? warp_eq[lane] : 0u;
+        g = __reduce_add_sync(0xffffffffu, lane < warp ? all_g : 0u);
+        e = __reduce_add_sync(0xffffffffu, lane < warp ? all_e : 0u);
+        if constexpr (CLUSTER) {
+            if (warp == 0) {
+                const uint32_t cta_g = __reduce_add_sync(0xffffffffu, all_g), cta_e = __reduce_add_sync(0xffffffffu, all_e);
+                if (lane == 0) {
+                    s_counts[0] = cta_g;
+                    s_counts[1] = cta_e;
+                }
+            }
+            cg::this_cluster().sync();            // every mass of the sequence has been read: mass_out may be the same array
+            for (int p = 0; p < part; ++p) {
+                const uint32_t *c = cg::this_cluster().map_shared_rank(&s_counts[0], p);
+                g += c[0];
+                e += c[1];
+            }
+        }
 #pragma unroll 2
-        for (int t0 = w0; t0 < w1; t0 += 32) {
-            const int t = t0 + lane;
+        for (int i0 = w0; i0 < w1; i0 += 32) {
+            const int i = i0 + lane;
             bool gt = false, eq = false;
-            const float w = t < w1 ? slice[t] : 0.0f;
-            if (t < w1) stays(t, w, gt, eq);
+            const float w = i < w1 ? from[i] : 0.0f;
+            if (i < w1) stays(i, w, gt, eq);
             const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
             const uint32_t e_me = e + __popc(be & below), to = g + __popc(bg & below) + min(e_me, need);
             if (gt || (eq && e_me < need)) {
-                kept[to] = t;
+                kept[to] = t0 + i;
                 mass_out[to] = w;
             }
             g += __popc(bg);
             e += __popc(be);
         }
+        if constexpr (CLUSTER) cg::this_cluster().sync();                      // nobody reads this CTA's counts any more
     } else {
         // a token per thread, tile by tile: what is written lies at or before the tokens that have been read, so mass_out may be
         // the same array
         uint32_t g = 0, e = 0;
 #pragma unroll 1
-        for (int t0 = 0; t0 < n; t0 += threads) {
-            const int t = t0 + tid;
+        for (int i0 = 0; i0 < n; i0 += threads) {
+            const int t = i0 + tid;
             bool gt = false, eq = false;
             float w = 0.0f;
             if (t < n) {
@@ -220,9 +299,9 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
         }
         __syncthreads();
     }
-    for (int j = m + tid; j < a.budget; j += threads) kept[j] = -1;
-    for (int t = m + tid; t < n; t += threads) mass_out[t] = 0.0f;
-    if (tid == 0 && l == 0 && h == 0) a.new_lens[b] = bad ? -1 : m;
+    for (int j = m + part * threads + tid; j < a.budget; j += parts * threads) kept[j] = -1;
+    for (int t = m + part * threads + tid; t < n; t += parts * threads) mass_out[t] = 0.0f;
+    if (tid == 0 && part == 0 && l == 0 && h == 0) a.new_lens[b] = bad ? -1 : m;
 }
 
 // A slab (K or V of a KV head) of one sequence; its CTAs take batches of rows in turn.
@@ -231,16 +310,11 @@ __global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a
 {
     constexpr int kMostRows = kMoveThreads / 2 * kInFlight;                   // of a batch: rows have at least two vectors
     __shared__ int2 rows[2][kMostRows];           // old and new row, of this round and the next; a new row of -1: nothing to move
-    const int vec = a.d / 8, at_once = kMoveThreads / vec, batch = at_once * kInFlight, tid = threadIdx.x;
-    const int r = tid / vec, c = tid - r * vec;
+    const int vec = a.d / 8, at_once = a.by_vec(kMoveThreads), batch = at_once * kInFlight, tid = threadIdx.x;
+    const int r = a.by_vec(tid), c = tid - r * vec;
     const bool live = r < at_once;
-    const int part = blockIdx.x % a.parts;
-    int x = blockIdx.x / a.parts;
-    const int half = x & 1;
-    x >>= 1;
-    const int h = x % a.Hkv;
-    x /= a.Hkv;
-    const int b = x % a.n_seqs, l = x / a.n_seqs;
+    const int slab_of = a.by_parts(blockIdx.x), part = blockIdx.x - slab_of * a.parts;
+    const int half = slab_of & 1, h = slab_of >> 1, b = blockIdx.y, l = blockIdx.z;
     const int32_t *kept = a.kept + (((int64_t)l * a.n_seqs + b) * a.Hkv + h) * a.budget;
     const int32_t *from = a.table + (int64_t)b * a.table_stride;
     const int32_t *to = IN_PLACE ? from : a.dst_table + (int64_t)b * a.dst_stride;
@@ -252,15 +326,15 @@ __global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a
     const int m = min(a.budget, n);
     if (IN_PLACE && m == n) return;               // every row stays where it is
     const int first = IN_PLACE ? part * batch : part * a.batches * batch, step = IN_PLACE ? a.parts * batch : batch;
-    const int rounds = IN_PLACE ? (m + step - 1) / step : min(a.batches, (m - first + batch - 1) / batch);
+    const int rounds = IN_PLACE ? (m + step - 1) / step : min(a.batches, max(0, m - first + batch - 1) / batch);
     auto look_up = [&](int k) {
         const int j0 = first + k * step;
         for (int i = tid; i < batch; i += kMoveThreads) {
             const int j = j0 + i;
             int2 x = make_int2(-1, -1);
             if (j < m) {
-                x.x = slot_row(from, a.chunk_len, a.n_slots, __ldcg(kept + j));
-                x.y = slot_row(to, a.chunk_len, a.n_slots, j);
+                x.x = slot_row(a, from, __ldcg(kept + j));
+                x.y = slot_row(a, to, j);
                 if (x.x < 0 || x.x == x.y) x.y = -1;
             }
             rows[k & 1][i] = x;
@@ -287,6 +361,25 @@ __global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a
     }
 }
 
+// A dependent launch (see launch_dependent) of clusters of `cluster` CTAs.
+static cudaError_t launch_cluster(void (*kernel)(EvictArgs), dim3 grid, int block, size_t smem, int cluster, cudaStream_t st, const EvictArgs &a)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 }  // namespace llms
 
 using namespace llms;
@@ -309,7 +402,7 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
         !aligned(kept, 4) || !aligned(new_lens, 4))
         return LLMS_ERR_MISALIGNED;
     const int64_t items = (int64_t)desc->n_layers * n_seqs * desc->n_kv_heads;
-    if (items > 0x7fffffff / 64) return LLMS_ERR_UNSUPPORTED;
+    if (items > 0x7fffffff / 64 || desc->n_layers > 65535) return LLMS_ERR_UNSUPPORTED;
     EvictArgs a{};
     a.mass = mass; a.mass_out = mass_out;
     a.kv = static_cast<uint16_t *>(kv);
@@ -319,15 +412,27 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     a.table_stride = table_stride; a.dst_stride = dst_stride;
     a.n_seqs = n_seqs; a.max_len = max_len; a.L = desc->n_layers; a.Hkv = desc->n_kv_heads; a.d = desc->head_dim;
     a.chunk_len = desc->chunk_len; a.n_slots = n_chunks(*desc);
+    a.by_chunk = Divisor(a.chunk_len);
+    a.by_vec = Divisor(a.d / 8);
     a.budget = budget; a.recent = recent;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // a thread of the selection has 32 masses, if that makes no more than 1024 threads
-    int threads = 128;
-    while (threads < 1024 && threads * 32 < max_len) threads *= 2;
-    a.in_smem = max_len <= kSliceTokens;
-    const size_t smem = a.in_smem ? round_up((uint64_t)max_len * 4, 16) : 0;
-    LLMS_CUDA_TRY(cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    LLMS_CUDA_TRY(launch_dependent(select_kernel, dim3((unsigned)items), dim3(threads), smem, st, a));
+    // Selection: as many threads as fit the GPU at once, but no fewer than 128 to a CTA and two masses to a thread
+    const int64_t room = (int64_t)sm_count() * 2048;
+    int threads = 1024;
+    while (threads > 128 && (items * threads > room || threads * 2 > max_len)) threads /= 2;
+    int parts = 1;
+    while (parts < kMaxCluster && items * threads * parts * 2 <= room && parts * threads * 4 <= max_len) parts *= 2;
+    int share = (max_len + parts - 1) / parts;
+    if (share > kSliceTokensShared) parts = 1, share = max_len;
+    const bool shared = parts > 1;
+    while ((1 << a.select_shift) < parts) ++a.select_shift;
+    while ((32 << a.warps_shift) < threads) ++a.warps_shift;
+    a.in_smem = shared || max_len <= kSliceTokens;
+    a.list_room = std::min(4096, std::max(256, (share / 8 + 1) & ~1));
+    const size_t smem = (shared ? 4 : 1) * kBins * 4 + (size_t)a.list_room * 8 + (a.in_smem ? round_up((uint64_t)share * 4, 16) : 0);
+    void (*select)(EvictArgs) = shared ? select_kernel<true> : select_kernel<false>;
+    LLMS_CUDA_TRY(cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    LLMS_CUDA_TRY(launch_cluster(select, dim3(a.Hkv * parts, n_seqs, a.L), threads, smem, parts, st, a));
 
     constexpr int kFillCtas = 592;
     const int batch = kMoveThreads / (a.d / 8) * kInFlight, most_batches = (most + batch - 1) / batch;
@@ -341,19 +446,8 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
         while (a.parts < kMaxCluster && items * 2 * a.parts < kFillCtas && a.parts < most_batches) a.parts *= 2;
         kernel = a.parts > 1 ? move_kernel<true, true> : move_kernel<true, false>;
     }
-    if (items * 2 * a.parts > 0x7fffffff) return LLMS_ERR_UNSUPPORTED;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(items * 2 * a.parts));
-    cfg.blockDim = dim3(kMoveThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = a.parts;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = !dst_table && a.parts > 1 ? 2 : 1;
-    LLMS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
+    if ((int64_t)a.Hkv * 2 * a.parts > 0x7fffffff) return LLMS_ERR_UNSUPPORTED;
+    a.by_parts = Divisor(a.parts);
+    LLMS_CUDA_TRY(launch_cluster(kernel, dim3(a.Hkv * 2 * a.parts, n_seqs, a.L), kMoveThreads, 0, dst_table ? 1 : a.parts, st, a));
     return LLMS_OK;
 }

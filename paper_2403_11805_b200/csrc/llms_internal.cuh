@@ -44,6 +44,22 @@ __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepco
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 #endif
 
+// Division of 0 .. 2^31 - 1 by a number known at launch: with l = ceil(log2 d) and m = floor(2^32 (2^l - d) / d) + 1 the quotient
+// is (high word of m * x, plus x) >> l (the multiply-and-shift method of Granlund and Montgomery); three instructions
+// where a division by a variable takes some twenty.
+struct Divisor {
+    uint32_t mul, shift;
+    Divisor() = default;
+    explicit Divisor(uint32_t d) : mul(0), shift(0)
+    {
+        while (shift < 31 && (1u << shift) < d) ++shift;
+        mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - d)) / d + 1);
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int operator()(int x) const { return (int)((__umulhi(mul, (uint32_t)x) + (uint32_t)x) >> shift); }
+#endif
+};
+
 inline uint64_t round_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 inline bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline bool is_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }

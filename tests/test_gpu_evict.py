@@ -64,6 +64,7 @@ SHAPES = {
     "dim_16": (dict(lens=[70], dim=16), 33, 1), "dim_112": (dict(lens=[70], dim=112, layers=2), 33, 1),
     "long": (dict(lens=[9001, 4096, 5], heads=2, dim=64), 3000, 100), "long_most": (dict(lens=[9001], heads=2, dim=64), 8999, 1),
     "longest": (dict(lens=[70000], heads=1, dim=16), 20000, 777),
+    "long_among_many": (dict(lens=[20001, 17000] + [i % 5 for i in range(150)], heads=1, dim=16), 9000, 300),
 }
 
 
