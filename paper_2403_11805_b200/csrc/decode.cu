@@ -103,6 +103,19 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
                  :: "r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
 }
+// Wait for the phase of the given parity to complete, all lanes of a warp together; false when it did not within the limit.
+__device__ __forceinline__ bool warp_wait(unsigned long long *bar, uint32_t parity)
+{
+    const uint32_t addr = smem_u32(bar);
+    uint32_t done = 0;
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(addr), "r"(parity) : "memory");
+        if (done) break;
+        if (i > 32) __nanosleep(64);
+    }
+    return __all_sync(0xffffffffu, done);
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, unsigned long long *bar)
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -204,14 +217,12 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t ring_addr = smem_u32(ring), q_addr = ring_addr + S::kStages * S::kStage;
     __shared__ unsigned long long full[S::kStages];
-    __shared__ uint32_t gave_up;
 
     const int lane = threadIdx.x, run = blockIdx.x;
     if (lane == 0) {
 #pragma unroll
         for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        gave_up = 0;
     }
     __syncwarp();
     grid_dependency_wait();
@@ -329,6 +340,8 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
 
         // ---- the arithmetic
         int stage = 0, phase = 0, done = w0;
+        bool lost = false;                                    // a copy did not arrive: no more are asked for, those on their way are
+                                                              // still waited for, and what has not arrived counts as NaN
         // addresses inside a tile: K as stored (rows = tokens), V transposed (rows = channels)
         const int k_row = lane & 15, v_row = (lane & 7) + ((lane >> 4) << 3);
         const uint32_t k_base = ring_addr + k_row * 128, v_base = ring_addr + S::kHalf + v_row * 128;
@@ -353,7 +366,8 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
                 }
                 fresh_slot = __ldg(a.table + (int64_t)c_seq * a.table_stride + a.by_chunk(c_s.len - 1));
             }
-            bool good = mbar_wait(&full[stage], phase, &gave_up);
+            bool good = idx < issued && warp_wait(&full[stage], phase);
+            lost |= !good;
             // query rows as the MMA's second operand; columns beyond the item's rows repeat others (nobody reads their
             // results), channels behind head_dim are 0 like K's there
             uint32_t qf[KS][NT][2];
@@ -388,7 +402,10 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
 
 #pragma unroll 1
             for (int tile = tile_begin; tile < tile_end; ++tile) {
-                if (tile != tile_begin) good = mbar_wait(&full[stage], phase, &gave_up);
+                if (tile != tile_begin) {
+                    good = done < issued && warp_wait(&full[stage], phase);
+                    lost |= !good;
+                }
                 const int tok0 = (c_s.tile0 + tile) * kTile;
                 const uint32_t at = stage * S::kStage;
                 const bool poison = !good || (poisoned >> stage & 1);
@@ -511,7 +528,7 @@ __global__ void __launch_bounds__(32) decode_kernel(const DecodeArgs a, const __
                 __syncwarp();
                 ++done;
 #pragma unroll 1
-                for (int s = 0; s < 2 && issued < w1 && issued < done + S::kStages; ++s) issue();   // two: one may have had to wait
+                for (int s = 0; s < 2 && !lost && issued < w1 && issued < done + S::kStages; ++s) issue();   // two: one may have had to wait
                 if (++stage == S::kStages) {
                     stage = 0;
                     phase ^= 1;

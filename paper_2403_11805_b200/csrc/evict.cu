@@ -2,7 +2,7 @@
 // rows and masses are closed up.
 //
 // Selection (select_kernel, a CTA, or where there are few of them a cluster of CTAs, per (layer, sequence, KV head)).  The masses'
-// order as unsigned keys (mass_key); the key of the quota-th heaviest candidate is found digit by digit, 11, 11 and 10 bits,
+// order as unsigned keys (key_of); the key of the quota-th heaviest candidate is found digit by digit, 11, 11 and 10 bits,
 // counting keys per digit value in shared memory (added up over the cluster's shared memories); keys above it stay, and of
 // those equal to it the first ones.  A last pass in the order of positions numbers the kept tokens.  The first digit has
 // sign, exponent and two bits of the fraction, so that masses that differ by powers of two - attention weights do - spread
@@ -46,23 +46,15 @@ struct EvictArgs {
     int parts, batches;                           // move: CTAs per slab; batches of rows a CTA takes (0: all, in place)
 };
 
-// Order of the masses as an unsigned key: larger mass, larger key; NaN and -inf are the same and lie below every other value,
-// -0 equals +0.  No key is above 0xff800000 (+inf) or below 0x007fffff.  odd: the sequence may have such values.
-__device__ __forceinline__ uint32_t mass_key(float m, bool odd)
+// What a mass is ranked by: NaN as -inf, -0 as +0.
+__device__ __forceinline__ float rank_value(float m) { return fmaxf(m, -INFINITY) + 0.0f; }
+// The order of these values as unsigned keys, 0x007fffff (-inf) to 0xff800000 (+inf), and back.
+__device__ __forceinline__ uint32_t key_of(float v)
 {
-    const uint32_t u = __float_as_uint(m);
-    uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
-    if (odd) {
-        if (k == 0x7fffffffu) k = 0x80000000u;
-        if ((u << 1) > 0xff000000u) k = 0x007fffffu;
-    }
-    return k;
+    const uint32_t u = __float_as_uint(v);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ bool is_odd(float m)
-{
-    const uint32_t u = __float_as_uint(m);
-    return u == 0x80000000u || (u << 1) > 0xff000000u;
-}
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key ^ (((int32_t)key >> 31) ? 0x80000000u : 0xffffffffu)); }
 
 __device__ __forceinline__ int slot_row(const EvictArgs &a, const int32_t *row, int t)
 {
@@ -95,10 +87,10 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
     const int n = bad ? 0 : len, m = min(a.budget, n), recent = min(a.recent, m), cand = n - recent, quota = m - recent;
     // this CTA's tokens, from t0 on, and how many of them are candidates
     const int share = CLUSTER ? (n + parts - 1) >> a.select_shift : n, t0 = CLUSTER ? min(n, part * share) : 0, count = min(n, t0 + share) - t0;
-    const int mine = max(0, min(count, cand - t0));
-    // Keys above `limit` stay, and the first `need` ones equal to it.  Nothing to rank: all candidates, or none
+    // (none if they all stay).  Values above the limit's stay, and the first `need` ones equal to it
+    const int mine = quota >= cand ? 0 : max(0, min(count, cand - t0));
     const bool ranked = quota > 0 && quota < cand;
-    uint32_t limit = quota == 0 ? 0xffffffffu : 0u, need = ranked ? quota : 0;
+    uint32_t limit = 0, need = ranked ? quota : 0;
     const float *from = a.in_smem ? slice : mass;
     // a warp's own tokens, for the passes in the order of positions
     const int warp_shift = a.warps_shift, each_warp = (((count + n_warps - 1) >> warp_shift) + 31) & ~31, w0 = min(count, warp * each_warp), w1 = min(count, w0 + each_warp);
@@ -107,15 +99,13 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
     if (tid == 0) s_listed = 0;
     if (tid < 32) warp_add[0][tid] = warp_add[1][tid] = 0;
     __syncthreads();                              // hist is cleared
-    bool odd = false;
 #pragma unroll 4
     for (int i = tid; i < count; i += threads) {
         const float w = __ldcg(mass + t0 + i);
         if (a.in_smem) slice[i] = w;
-        odd |= is_odd(w);
-        if (ranked && i < mine) atomicAdd(&hist[mass_key(w, true) >> 21], 1u);
+        if (ranked && i < mine) atomicAdd(&hist[key_of(rank_value(w)) >> 21], 1u);
     }
-    odd = __syncthreads_or(odd);
+    __syncthreads();
     bool listed = false;
     if (ranked) {
 #pragma unroll 1
@@ -170,17 +160,20 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
             if (shift == 21) {
                 listed = s_bin <= (uint32_t)a.list_room;                       // the whole cluster's: the same for all its CTAs
                 if (listed) {
-#pragma unroll 2
+                    // values from `low` on have the limit's digit, from `high` on a higher one (none if that is no number)
+                    const float high = value_of((want + 1) << 21), low = want << 21 < 0x007fffffu ? -INFINITY : value_of(want << 21);
+#pragma unroll 4
                     for (int i0 = w0; i0 < w1; i0 += 32) {
                         const int i = i0 + lane;
-                        const uint32_t k = i < mine ? mass_key(from[i], odd) : 0u;
-                        n_gt += i < w1 && (i >= mine || k >> 21 > want);
-                        const uint32_t bl = __ballot_sync(0xffffffffu, i < mine && i < w1 && k >> 21 == want);
+                        const float v = i < w1 ? fmaxf(from[i], -INFINITY) : 0.0f;
+                        const bool above = i >= mine || v >= high;
+                        n_gt += above && i < w1;
+                        const uint32_t bl = __ballot_sync(0xffffffffu, !above && v >= low);
                         if (bl) {
                             uint32_t at = 0;
                             if (lane == 0) at = atomicAdd(&s_listed, __popc(bl));
                             at = __shfl_sync(0xffffffffu, at, 0) + __popc(bl & below);
-                            if (bl >> lane & 1) list[at] = make_uint2(k, i);
+                            if (bl >> lane & 1) list[at] = make_uint2(key_of(v + 0.0f), i);
                         }
                     }
                     __syncthreads();
@@ -195,18 +188,18 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
             } else {
 #pragma unroll 8
                 for (int i = tid; i < mine; i += threads) {
-                    const uint32_t k = mass_key(from[i], odd);
+                    const uint32_t k = key_of(rank_value(from[i]));
                     if (k >> shift == want) atomicAdd(&hist[(k >> next) & ((1u << bits) - 1u)], 1u);
                 }
             }
             __syncthreads();
         }
     }
-    const bool everything = quota >= cand;
+    const float border = ranked ? value_of(limit) : INFINITY;                  // nothing to rank: no candidate stays
     auto stays = [&](int i, float w, bool &gt, bool &eq) {                     // token t0 + i
-        const uint32_t k = mass_key(w, odd);
-        gt = i >= mine || everything || k > limit;
-        eq = !gt && need > 0 && k == limit;
+        const float v = fmaxf(w, -INFINITY);
+        gt = i >= mine || v > border;
+        eq = !gt && v == border;
     };
     if (CLUSTER || a.in_smem || a.mass != a.mass_out) {
         // a warp takes neighbouring tokens, 32 at a time: it counts its ones, then numbers them in the order of positions
@@ -258,13 +251,18 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
             const float w = i < w1 ? from[i] : 0.0f;
             if (i < w1) stays(i, w, gt, eq);
             const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
-            const uint32_t e_me = e + __popc(be & below), to = g + __popc(bg & below) + min(e_me, need);
-            if (gt || (eq && e_me < need)) {
+            uint32_t e_me = e;
+            if (be) {                             // few tokens are equal to the limit
+                e_me += __popc(be & below);
+                gt |= eq && e_me < need;
+                e += __popc(be);
+            }
+            const uint32_t to = g + __popc(bg & below) + min(e_me, need);
+            if (gt) {
                 kept[to] = t0 + i;
                 mass_out[to] = w;
             }
             g += __popc(bg);
-            e += __popc(be);
         }
         if constexpr (CLUSTER) cg::this_cluster().sync();                      // nobody reads this CTA's counts any more
     } else {
@@ -395,6 +393,7 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     if (n_seqs == 0) return LLMS_OK;
     if (!kv || !mass || !chunk_table || !lens || !mass_out || !kept || !new_lens || new_lens == lens) return LLMS_ERR_INVALID_ARG;
     if (table_stride < 1 || (int64_t)table_stride * desc->chunk_len < max_len || mass_stride < max_len) return LLMS_ERR_INVALID_ARG;
+    if (dst_table == chunk_table && dst_stride == table_stride) dst_table = nullptr;   // the sequence's own chunks
     const int most = budget < max_len ? budget : max_len;
     if (dst_table && (dst_stride < 1 || (int64_t)dst_stride * desc->chunk_len < most)) return LLMS_ERR_INVALID_ARG;
     if (!aligned(kv, 16)) return LLMS_ERR_MISALIGNED;
@@ -438,7 +437,7 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     const int batch = kMoveThreads / (a.d / 8) * kInFlight, most_batches = (most + batch - 1) / batch;
     void (*kernel)(EvictArgs);
     if (dst_table) {
-        a.batches = 8;
+        a.batches = 4;
         a.parts = (most_batches + a.batches - 1) / a.batches;
         kernel = move_kernel<false, false>;
     } else {

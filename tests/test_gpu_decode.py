@@ -267,6 +267,34 @@ def test_captured_replayed_and_on_another_stream():
         assert torch.equal(outs[0], outs[1])
 
 
+def test_largest_batch():
+    """4096 sequences, most of them empty or a few tokens long."""
+    bt = Batch([(i * 7919) % 5 if i % 3 else 0 for i in range(4095)] + [70], heads=1, dim=16, group=2, seed=17)
+    check(bt, append=True, mass="add")
+
+
+def test_two_streams_at_once():
+    """Two batches in one pool, on two streams with a workspace each, many calls in flight."""
+    both = [Batch([900, 30, 0, 411], heads=2, group=4, dim=128, seed=s) for s in (41, 42)]
+    streams = [torch.cuda.Stream() for _ in both]
+    jobs = []
+    for bt in both:
+        d = desc_of(bt)
+        jobs.append((d, bt.kv.cuda(), bt.q.contiguous().cuda(), bt.table.cuda(), torch.tensor(bt.lens, dtype=torch.int32).cuda(),
+                     [torch.empty(4, 8, 128, dtype=F16, device="cuda") for _ in range(20)], workspace(d, 4, 900), bt.k_new.contiguous().cuda(),
+                     bt.v_new.contiguous().cuda()))
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s, (d, kv, q, table, lens, outs, ws, k, v) in zip(streams, jobs):
+            B.decode_attention(d, 0, kv, q, table, lens, 900, outs[i], ws, k_new=k, v_new=v, stream=s)
+    torch.cuda.synchronize()
+    for bt, job in zip(both, jobs):
+        want, _, _, _, (ot, _, _) = attend(bt, append=True)
+        for o in job[5]:
+            assert torch.equal(o, job[5][0])
+        assert ((job[5][0].cpu().double() - want).abs() <= ot).all()
+
+
 def test_refusals():
     bt = Batch([20, 30], group=2, seed=1)
     d = desc_of(bt)

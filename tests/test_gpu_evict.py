@@ -105,6 +105,16 @@ def test_dst_table_may_be_the_table_itself():
     assert torch.equal(bits(a[3]), bits(want[3]))
 
 
+def test_the_table_as_its_own_destination_is_in_place():
+    bt = Batch([90, 40, 500], seed=5)
+    dev, lens = bt.table.cuda(), torch.tensor(bt.lens, dtype=torch.int32).cuda()
+    kept, new_lens = torch.zeros(1, 3, 2, 33, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    kv = bt.kv.cuda()
+    B.evict_tokens(desc_of(bt), kv, bt.mass.cuda(), dev, lens, 500, 33, 4, kept, new_lens, dst_table=dev)
+    want = evict(bt, bt.mass, 33, 4)
+    assert torch.equal(kept.cpu(), want[0]) and torch.equal(bits(kv.cpu()), bits(want[3]))
+
+
 def test_in_place_twice_and_repeatable():
     bt = Batch([3000, 777], heads=4, dim=128, seed=6, layers=2)
     first = call(bt, bt.mass, 1500, 64)
