@@ -370,6 +370,7 @@ DTYPE_F16, DTYPE_BF16 = 0, 1
 # These calls come once per layer and token, so their argument checks are written as one condition each; what is wrong is
 # worked out only after it has failed.
 _torch = None
+_CACHE_TYPES = {}
 
 
 def _current(stream):
@@ -378,19 +379,12 @@ def _current(stream):
     if _torch is None:
         import torch
         torch.cuda.init()
+        _CACHE_TYPES.update({torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16})
         _torch = torch
     device = _torch._C._cuda_getDevice()
     if stream is None:
         return device, _torch._C._cuda_getCurrentRawStream(device)
     return device, stream if isinstance(stream, int) else stream.cuda_stream
-
-
-def _is_rows(x, n, heads, d, dtype, device):
-    """[n, heads, d] with a sequence's heads side by side; the sequences may be any number of elements apart."""
-    if x.shape != (n, heads, d) or x.dtype is not dtype or x.get_device() != device:
-        return False
-    _, head, channel = x.stride()
-    return channel == 1 and (head == d or heads == 1)
 
 
 def _is_whole(x, shape, dtype, device):
@@ -427,29 +421,36 @@ def decode_attention(desc, layer, kv, q, chunk_table, lens, max_len, out, worksp
     of one projection's output.  All tensors on the current device."""
     what = "llms_decode_attention"
     device, stream = _current(stream)
-    n, d, hq, hk, dtype = lens.shape[0], desc.head_dim, desc.n_q_heads, desc.n_kv_heads, kv.dtype
-    f32 = _torch.float32
-    if dtype is _torch.float16:
-        code = DTYPE_F16
-    elif dtype is _torch.bfloat16:
-        code = DTYPE_BF16
-    else:
+    n, d, hq, hk, dtype = lens.numel(), desc.head_dim, desc.n_q_heads, desc.n_kv_heads, kv.dtype
+    i32, f32 = _torch.int32, _torch.float32
+    code = _CACHE_TYPES.get(dtype)
+    if code is None:
         raise LlmsError(ERR_UNSUPPORTED, f"{what}: a cache of {dtype} (float16 and bfloat16 are taken)")
-    if not (_is_batch(chunk_table, lens, device) and kv.get_device() == device and workspace.get_device() == device
-            and _is_rows(q, n, hq, d, dtype, device) and _is_whole(out, (n, hq, d), dtype, device)
+    q_stride, q_head, q_channel = q.stride() if q.dim() == 3 else (0, 0, 0)
+    table_stride, table_entry = chunk_table.stride() if chunk_table.dim() == 2 else (0, 0)
+    chunks = chunk_table.shape[-1]
+    if not (lens.dtype is i32 and lens.get_device() == device and lens.is_contiguous() and lens.dim() == 1
+            and chunk_table.dtype is i32 and chunk_table.get_device() == device and (table_entry == 1 or chunks == 1)
+            and chunk_table.shape[0] == n and kv.get_device() == device and workspace.get_device() == device
+            and q.dtype is dtype and q.get_device() == device and q.shape == (n, hq, d) and q_channel == 1 and (q_head == d or hq == 1)
+            and out.dtype is dtype and out.get_device() == device and out.shape == (n, hq, d) and out.is_contiguous()
             and (lse is None or _is_whole(lse, (n, hq), f32, device))):
         _refuse(what, device, f"kv on this device, chunk_table int32 [{n}, chunks], lens int32 [{n}], q and out [{n}, {hq}, {d}] of kv's type, "
                 f"lse float32 [{n}, {hq}]", kv=kv, chunk_table=chunk_table, lens=lens, q=q, out=out, lse=lse, workspace=workspace)
-    chunks = chunk_table.shape[1]
+    if n <= 1:
+        q_stride, table_stride = hq * d, chunks
     if chunks * desc.chunk_len < max_len:
         _refuse(what, device, f"max_len {max_len} is more than a table row's chunks of {desc.chunk_len} hold", chunk_table=chunk_table)
     k_ptr = v_ptr = in_ptr = out_ptr = None
     new_stride = mass_stride = 0
     if k_new is not None or v_new is not None:
-        if not (k_new is not None and v_new is not None and _is_rows(k_new, n, hk, d, dtype, device)
-                and _is_rows(v_new, n, hk, d, dtype, device) and (n == 1 or k_new.stride(0) == v_new.stride(0))):
-            _refuse(what, device, f"k_new and v_new together, [{n}, {hk}, {d}] of kv's type with the same strides", k_new=k_new, v_new=v_new)
-        k_ptr, v_ptr, new_stride = k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0) if n > 1 else hk * d
+        if not (k_new is not None and v_new is not None and k_new.shape == (n, hk, d) == v_new.shape and k_new.dtype is dtype
+                and v_new.dtype is dtype and k_new.get_device() == device and v_new.get_device() == device):
+            _refuse(what, device, f"k_new and v_new together, [{n}, {hk}, {d}] of kv's type", k_new=k_new, v_new=v_new)
+        strides = k_new.stride()
+        if not (strides[2] == 1 and (strides[1] == d or hk == 1)) or (strides != v_new.stride() and (n > 1 or not v_new.is_contiguous())):
+            _refuse(what, device, "a sequence's heads of k_new and v_new side by side, both with the same strides", k_new=k_new, v_new=v_new)
+        k_ptr, v_ptr, new_stride = k_new.data_ptr(), v_new.data_ptr(), strides[0] if n > 1 else hk * d
     if mass_out is not None or mass_in is not None:
         mass_stride = 0 if mass_out is None else mass_out.shape[-1]
         if not (mass_out is not None and _is_whole(mass_out, (n, hk, mass_stride), f32, device)
@@ -457,10 +458,9 @@ def decode_attention(desc, layer, kv, q, chunk_table, lens, max_len, out, worksp
             _refuse(what, device, f"mass_out float32 [{n}, {hk}, >= {max_len}], mass_in none or like it", mass_in=mass_in, mass_out=mass_out)
         out_ptr, in_ptr = mass_out.data_ptr(), None if mass_in is None else mass_in.data_ptr()
     rc = (_lib or lib()).llms_decode_attention(
-        C.addressof(desc), code, layer, kv.data_ptr(), q.data_ptr(), q.stride(0) if n > 1 else hq * d, k_ptr, v_ptr, new_stride,
-        chunk_table.data_ptr(), chunk_table.stride(0) if n > 1 else chunks, lens.data_ptr(), n, max_len, window,
-        d ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(), in_ptr, out_ptr, mass_stride,
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+        C.addressof(desc), code, layer, kv.data_ptr(), q.data_ptr(), q_stride, k_ptr, v_ptr, new_stride, chunk_table.data_ptr(), table_stride,
+        lens.data_ptr(), n, max_len, window, d ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+        in_ptr, out_ptr, mass_stride, workspace.data_ptr(), workspace.nbytes, stream)
     if rc < 0:
         raise LlmsError(rc, what)
 
