@@ -86,24 +86,36 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
     const bool bad = len < 0 || len > a.max_len;
     const int n = bad ? 0 : len, m = min(a.budget, n), recent = min(a.recent, m), cand = n - recent, quota = m - recent;
     // this CTA's tokens, from t0 on, and how many of them are candidates
-    const int share = CLUSTER ? (n + parts - 1) >> a.select_shift : n, t0 = CLUSTER ? min(n, part * share) : 0, count = min(n, t0 + share) - t0;
+    const int share = CLUSTER ? (((n + parts - 1) >> a.select_shift) + 3) & ~3 : n, t0 = CLUSTER ? min(n, part * share) : 0, count = min(n, t0 + share) - t0;
     // (none if they all stay).  Values above the limit's stay, and the first `need` ones equal to it
     const int mine = quota >= cand ? 0 : max(0, min(count, cand - t0));
     const bool ranked = quota > 0 && quota < cand;
     uint32_t limit = 0, need = ranked ? quota : 0;
     const float *from = a.in_smem ? slice : mass;
+    // four neighbouring masses (what lies behind the last one is -inf and counts nowhere)
+    const bool wide = a.in_smem || (reinterpret_cast<uintptr_t>(mass) & 15) == 0;                // t0 is a multiple of four
+    auto four = [&](const float *src, int i, bool vector) {
+        if (vector && i + 4 <= count) return *reinterpret_cast<const float4 *>(src + i);
+        return make_float4(i < count ? src[i] : -INFINITY, i + 1 < count ? src[i + 1] : -INFINITY, i + 2 < count ? src[i + 2] : -INFINITY,
+                           i + 3 < count ? src[i + 3] : -INFINITY);
+    };
     // a warp's own tokens, for the passes in the order of positions
-    const int warp_shift = a.warps_shift, each_warp = (((count + n_warps - 1) >> warp_shift) + 31) & ~31, w0 = min(count, warp * each_warp), w1 = min(count, w0 + each_warp);
+    const int warp_shift = a.warps_shift, each_warp = (((count + n_warps - 1) >> warp_shift) + 127) & ~127, w0 = min(count, warp * each_warp), w1 = min(count, w0 + each_warp);
     uint32_t n_gt = 0, n_eq = 0;                  // of the warp's tokens: above the limit, equal to it
-    const uint32_t below = (1u << lane) - 1u;
     if (tid == 0) s_listed = 0;
     if (tid < 32) warp_add[0][tid] = warp_add[1][tid] = 0;
     __syncthreads();                              // hist is cleared
-#pragma unroll 4
-    for (int i = tid; i < count; i += threads) {
-        const float w = __ldcg(mass + t0 + i);
-        if (a.in_smem) slice[i] = w;
-        if (ranked && i < mine) atomicAdd(&hist[key_of(rank_value(w)) >> 21], 1u);
+    const bool aligned_rows = (reinterpret_cast<uintptr_t>(mass) & 15) == 0;
+#pragma unroll 2
+    for (int i = 4 * tid; i < count; i += 4 * threads) {
+        const float4 x = four(mass + t0, i, aligned_rows);
+        if (a.in_smem) *reinterpret_cast<float4 *>(slice + i) = x;
+        if (ranked) {
+            const float w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i + j < mine) atomicAdd(&hist[key_of(rank_value(w[j])) >> 21], 1u);
+        }
     }
     __syncthreads();
     bool listed = false;
@@ -162,18 +174,16 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
                 if (listed) {
                     // values from `low` on have the limit's digit, from `high` on a higher one (none if that is no number)
                     const float high = value_of((want + 1) << 21), low = want << 21 < 0x007fffffu ? -INFINITY : value_of(want << 21);
-#pragma unroll 4
-                    for (int i0 = w0; i0 < w1; i0 += 32) {
-                        const int i = i0 + lane;
-                        const float v = i < w1 ? fmaxf(from[i], -INFINITY) : 0.0f;
-                        const bool above = i >= mine || v >= high;
-                        n_gt += above && i < w1;
-                        const uint32_t bl = __ballot_sync(0xffffffffu, !above && v >= low);
-                        if (bl) {
-                            uint32_t at = 0;
-                            if (lane == 0) at = atomicAdd(&s_listed, __popc(bl));
-                            at = __shfl_sync(0xffffffffu, at, 0) + __popc(bl & below);
-                            if (bl >> lane & 1) list[at] = make_uint2(key_of(v + 0.0f), i);
+#pragma unroll 2
+                    for (int i = w0 + 4 * lane; i < w1; i += 128) {
+                        const float4 x = four(from, i, wide);
+                        const float w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float v = fmaxf(w[j], -INFINITY);
+                            const bool above = i + j >= mine || v >= high;
+                            n_gt += above && i + j < w1;
+                            if (!above && v >= low) list[atomicAdd(&s_listed, 1u)] = make_uint2(key_of(v + 0.0f), i + j);
                         }
                     }
                     __syncthreads();
@@ -209,12 +219,16 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
                 if (x.x >= limit) atomicAdd(&warp_add[x.x == limit][x.y / (uint32_t)each_warp], 1u);
             }
         } else {
-#pragma unroll 4
-            for (int i = w0 + lane; i < w1; i += 32) {
-                bool gt, eq;
-                stays(i, from[i], gt, eq);
-                n_gt += gt;
-                n_eq += eq;
+            for (int i = w0 + 4 * lane; i < w1; i += 128) {
+                const float4 x = four(from, i, wide);
+                const float w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    bool gt, eq;
+                    stays(i + j, w[j], gt, eq);
+                    n_gt += gt && i + j < w1;
+                    n_eq += eq && i + j < w1;
+                }
             }
         }
         __syncthreads();
@@ -244,30 +258,53 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
                 e += c[1];
             }
         }
-#pragma unroll 2
-        for (int i0 = w0; i0 < w1; i0 += 32) {
-            const int i = i0 + lane;
-            bool gt = false, eq = false;
-            const float w = i < w1 ? from[i] : 0.0f;
-            if (i < w1) stays(i, w, gt, eq);
-            const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
-            uint32_t e_me = e;
-            if (be) {                             // few tokens are equal to the limit
-                e_me += __popc(be & below);
-                gt |= eq && e_me < need;
-                e += __popc(be);
+        uint32_t first = g + min(e, need);        // where the warp's first token goes that stays
+#pragma unroll 1
+        for (int i0 = w0; i0 < w1; i0 += 128) {
+            const int i = i0 + 4 * lane;
+            const float4 x = four(from, i, wide);
+            const float w[4] = {x.x, x.y, x.z, x.w};
+            uint32_t gts = 0, eqs = 0;            // bit j: token i + j is above the limit, equal to it
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                bool gt, eq;
+                stays(i + j, w[j], gt, eq);
+                gts |= (gt && i + j < w1 ? 1u : 0u) << j;
+                eqs |= (eq && i + j < w1 ? 1u : 0u) << j;
             }
-            const uint32_t to = g + __popc(bg & below) + min(e_me, need);
-            if (gt) {
-                kept[to] = t0 + i;
-                mass_out[to] = w;
+            if (__any_sync(0xffffffffu, eqs)) {   // few tokens are equal to the limit: those that stay join the others
+                uint32_t upto = __popc(eqs);
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const uint32_t up = __shfl_up_sync(0xffffffffu, upto, d);
+                    if (lane >= d) upto += up;
+                }
+                uint32_t e_me = e + upto - __popc(eqs);
+                e += __shfl_sync(0xffffffffu, upto, 31);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (eqs >> j & 1) gts |= (e_me++ < need ? 1u : 0u) << j;
             }
-            g += __popc(bg);
+            uint32_t upto = __popc(gts);
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const uint32_t up = __shfl_up_sync(0xffffffffu, upto, d);
+                if (lane >= d) upto += up;
+            }
+            uint32_t to = first + upto - __popc(gts);
+            first += __shfl_sync(0xffffffffu, upto, 31);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (gts >> j & 1) {
+                    kept[to] = t0 + i + j;
+                    mass_out[to++] = w[j];
+                }
         }
         if constexpr (CLUSTER) cg::this_cluster().sync();                      // nobody reads this CTA's counts any more
     } else {
         // a token per thread, tile by tile: what is written lies at or before the tokens that have been read, so mass_out may be
         // the same array
+        const uint32_t below = (1u << lane) - 1u;
         uint32_t g = 0, e = 0;
 #pragma unroll 1
         for (int i0 = 0; i0 < n; i0 += threads) {
@@ -421,7 +458,7 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     while (threads > 128 && (items * threads > room || threads * 2 > max_len)) threads /= 2;
     int parts = 1;
     while (parts < kMaxCluster && items * threads * parts * 2 <= room && parts * threads * 4 <= max_len) parts *= 2;
-    int share = (max_len + parts - 1) / parts;
+    int share = ((max_len + parts - 1) / parts + 3) & ~3;
     if (share > kSliceTokensShared) parts = 1, share = max_len;
     const bool shared = parts > 1;
     while ((1 << a.select_shift) < parts) ++a.select_shift;
