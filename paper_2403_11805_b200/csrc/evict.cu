@@ -28,7 +28,8 @@ namespace cg = cooperative_groups;
 constexpr int kSliceTokens = 16384;               // masses that a CTA holds in shared memory; of longer sequences it reads them again,
 constexpr int kSliceTokensShared = 49152;         // but a cluster's CTAs hold theirs
 constexpr int kBins = 2048;
-constexpr int kMoveThreads = 256, kInFlight = 4;  // 16-byte vectors a thread has in flight
+constexpr int kMoveThreads = 256;
+__host__ __device__ constexpr int in_flight(bool cluster) { return cluster ? 8 : 4; }   // 16-byte vectors of a thread
 constexpr int kMaxCluster = 8;
 
 struct EvictArgs {
@@ -343,7 +344,7 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
 template <bool IN_PLACE, bool CLUSTER>
 __global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a)
 {
-    constexpr int kMostRows = kMoveThreads / 2 * kInFlight;                   // of a batch: rows have at least two vectors
+    constexpr int kInFlight = in_flight(CLUSTER), kMostRows = kMoveThreads / 2 * kInFlight;                   // of a batch: rows have at least two vectors
     __shared__ int2 rows[2][kMostRows];           // old and new row, of this round and the next; a new row of -1: nothing to move
     const int vec = a.d / 8, at_once = a.by_vec(kMoveThreads), batch = at_once * kInFlight, tid = threadIdx.x;
     const int r = a.by_vec(tid), c = tid - r * vec;
@@ -470,8 +471,8 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     LLMS_CUDA_TRY(cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     LLMS_CUDA_TRY(launch_cluster(select, dim3(a.Hkv * parts, n_seqs, a.L), threads, smem, parts, st, a));
 
-    constexpr int kFillCtas = 592;
-    const int batch = kMoveThreads / (a.d / 8) * kInFlight, most_batches = (most + batch - 1) / batch;
+    constexpr int kFillCtas = 296;                // in place, a slab is shared by a cluster until there are so many CTAs (see move_kernel)
+    const int batch = kMoveThreads / (a.d / 8) * in_flight(false), most_batches = (most + batch - 1) / batch;
     void (*kernel)(EvictArgs);
     if (dst_table) {
         a.batches = 4;
