@@ -397,25 +397,6 @@ __global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a
     }
 }
 
-// A dependent launch (see launch_dependent) of clusters of `cluster` CTAs.
-static cudaError_t launch_cluster(void (*kernel)(EvictArgs), dim3 grid, int block, size_t smem, int cluster, cudaStream_t st, const EvictArgs &a)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(block);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a);
-}
-
 }  // namespace llms
 
 using namespace llms;
@@ -469,7 +450,7 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     const size_t smem = (shared ? 4 : 1) * kBins * 4 + (size_t)a.list_room * 8 + (a.in_smem ? round_up((uint64_t)share * 4, 16) : 0);
     void (*select)(EvictArgs) = shared ? select_kernel<true> : select_kernel<false>;
     LLMS_CUDA_TRY(cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    LLMS_CUDA_TRY(launch_cluster(select, dim3(a.Hkv * parts, n_seqs, a.L), threads, smem, parts, st, a));
+    LLMS_CUDA_TRY(launch_dependent_cluster(select, dim3(a.Hkv * parts, n_seqs, a.L), dim3(threads), smem, parts, st, a));
 
     constexpr int kFillCtas = 296;                // in place, a slab is shared by a cluster until there are so many CTAs (see move_kernel)
     const int batch = kMoveThreads / (a.d / 8) * in_flight(false), most_batches = (most + batch - 1) / batch;
@@ -485,6 +466,6 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     }
     if ((int64_t)a.Hkv * 2 * a.parts > 0x7fffffff) return LLMS_ERR_UNSUPPORTED;
     a.by_parts = Divisor(a.parts);
-    LLMS_CUDA_TRY(launch_cluster(kernel, dim3(a.Hkv * 2 * a.parts, n_seqs, a.L), kMoveThreads, 0, dst_table ? 1 : a.parts, st, a));
+    LLMS_CUDA_TRY(launch_dependent_cluster(kernel, dim3(a.Hkv * 2 * a.parts, n_seqs, a.L), dim3(kMoveThreads), 0, dst_table ? 1 : a.parts, st, a));
     return LLMS_OK;
 }
