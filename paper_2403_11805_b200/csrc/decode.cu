@@ -361,15 +361,37 @@ __device__ __forceinline__ void join_item(const DecodeArgs &a, unsigned char *ri
         const float *v = a.logits + at * a.max_len * a.group, *in = a.mass_in ? a.mass_in + at * a.mass_stride : nullptr;
         float *out = a.mass_out + at * a.mass_stride;
         const int t1 = min(s.len, (s.tile0 + w1) * kTile);
-        for (int t = max(s.first, (s.tile0 + w0) * kTile) + lane; t < t1; t += 32) {
-            float w = 0.0f;
-            for (int r = 0; r < have; ++r) {
-                const float lse = s_lse[warp][r];
-                w += lse == -INFINITY ? 0.0f : exp2_fast(v[(int64_t)t * a.group + r] - lse);
+        constexpr int kAtOnce = 4;                            // tokens of a lane whose loads are under way together
+        auto put = [&](int t0, int end, int step, auto weight) {               // tokens t0, t0 + step, ...
+#pragma unroll 1
+            for (int t = t0; t < end; t += kAtOnce * step) {
+                float w[kAtOnce];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) {
+                    const int u = t + i * step;
+                    w[i] = u < end ? weight(u) : 0.0f;
+                    if (in && u < end) w[i] = in[u] + w[i];
+                }
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i)
+                    if (t + i * step < end) out[t + i * step] = w[i];
             }
-            out[t] = (in ? in[t] : 0.0f) + w;
-        }
-        for (int t = part * kThreads + tid; t < s.first; t += ctas * kThreads) out[t] = in ? in[t] : 0.0f;   // before the window
+        };
+        auto one = [&](float x, int r) { return s_lse[warp][r] == -INFINITY ? 0.0f : exp2_fast(x - s_lse[warp][r]); };
+        put(max(s.first, (s.tile0 + w0) * kTile) + lane, t1, 32, [&](int t) {
+            const float *x = v + (int64_t)t * a.group;
+            float w = 0.0f;
+            if ((have & 3) == 0) {                            // (have is the group here)
+                for (int r = 0; r < have; r += 4) {
+                    const float4 y = *reinterpret_cast<const float4 *>(x + r);
+                    w += (one(y.x, r) + one(y.y, r + 1)) + (one(y.z, r + 2) + one(y.w, r + 3));
+                }
+            } else {
+                for (int r = 0; r < have; ++r) w += one(x[r], r);
+            }
+            return w;
+        });
+        if (in != out) put(part * kThreads + tid, s.first, ctas * kThreads, [&](int) { return 0.0f; });   // before the window
     }
     cluster.sync();                                           // nobody reads this CTA's pieces any more
 }
@@ -657,9 +679,16 @@ __global__ void __launch_bounds__(ITEM ? kItemWarps * 32 : 32) decode_kernel(con
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int t = tok0 + (lane >> 2) + (i >> 1) * 8;
-                            if (nt * 8 + (lane & 3) * 2 + (i & 1) < have && t < c_s.len) logits[(int64_t)t * a.group + nt * 8 + (i & 1)] = s[nt][i];
+                        for (int i = 0; i < 4; i += 2) {
+                            const int t = tok0 + (lane >> 2) + i * 4, r = nt * 8 + (lane & 3) * 2;
+                            float *to = logits + (int64_t)t * a.group + nt * 8;
+                            if (t >= c_s.len || r >= have) continue;
+                            if ((a.group & 1) == 0) {
+                                *reinterpret_cast<float2 *>(to) = make_float2(s[nt][i], s[nt][i + 1]);
+                            } else {
+                                to[0] = s[nt][i];
+                                if (r + 1 < have) to[1] = s[nt][i + 1];
+                            }
                         }
                 }
 #pragma unroll
