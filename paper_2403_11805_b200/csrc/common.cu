@@ -2,7 +2,7 @@
 #include <stdio.h>
 #include <string.h>
 
-#include "llms_internal.cuh"
+#include "paged.cuh"
 
 namespace llms {
 

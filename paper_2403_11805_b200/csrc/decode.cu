@@ -29,7 +29,7 @@
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
-#include "llms_internal.cuh"
+#include "paged.cuh"
 #include "tma.cuh"
 
 namespace llms {

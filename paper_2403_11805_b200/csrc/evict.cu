@@ -19,7 +19,7 @@
 
 #include <cooperative_groups.h>
 
-#include "llms_internal.cuh"
+#include "paged.cuh"
 
 namespace llms {
 

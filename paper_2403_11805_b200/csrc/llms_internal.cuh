@@ -25,49 +25,24 @@ void set_cuda_error(cudaError_t e, const char *where);
 // call grid_dependency_wait() before it touches anything its predecessor wrote: that returns when the predecessor has
 // completed and its writes are visible.  Both calls do nothing in a kernel that was launched the ordinary way.
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_dependent_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st,
-                                            Args &&...args)                    // grid.x a multiple of `cluster`, the CTAs of a cluster
+inline cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args &&...args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[2];
+    cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
-template <typename... KArgs, typename... Args>
-inline cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args &&...args)
-{
-    return launch_dependent_cluster(kernel, grid, block, smem, 1, st, static_cast<Args &&>(args)...);
 }
 #ifdef __CUDACC__
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 #endif
-
-// Division of 0 .. 2^31 - 1 by a number known at launch: with l = ceil(log2 d) and m = floor(2^32 (2^l - d) / d) + 1 the quotient
-// is (high word of m * x, plus x) >> l (the multiply-and-shift method of Granlund and Montgomery); three instructions
-// where a division by a variable takes some twenty.
-struct Divisor {
-    uint32_t mul, shift;
-    Divisor() = default;
-    explicit Divisor(uint32_t d) : mul(0), shift(0)
-    {
-        while (shift < 31 && (1u << shift) < d) ++shift;
-        mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - d)) / d + 1);
-    }
-#ifdef __CUDACC__
-    __device__ __forceinline__ int operator()(int x) const { return (int)((__umulhi(mul, (uint32_t)x) + (uint32_t)x) >> shift); }
-#endif
-};
 
 inline uint64_t round_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 inline bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -86,8 +61,6 @@ inline uint64_t groups_per_chunk(const llms_kv_desc &d) { return (uint64_t)slabs
 int check_desc(const llms_kv_desc *d);
 // Shape + alignment checks for the codec kernels (vector loads need 16-byte aligned slabs).
 int check_desc_codec(const llms_kv_desc *d);
-// Shape checks of the calls that use a paged cache: a pool the codec could take, with head_dim up to 256, and a batch.
-int check_paged(const llms_kv_desc *d, int n_seqs, int max_len);
 inline int check_bits(int b) { return (b == 1 || b == 2 || b == 4 || b == 8) ? LLMS_OK : LLMS_ERR_BAD_BITS; }
 
 // Number of SMs of the current device (cached per device).
