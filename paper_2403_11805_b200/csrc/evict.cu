@@ -15,6 +15,14 @@
 // range of rows.  In place a kept row's new position never lies behind its old one: a CTA that goes up in batches, each read
 // completely before it is written, never overwrites a row that it has yet to read.  Where there are few slabs a cluster
 // shares one, batch by batch.
+//
+// One kernel or two.  Where an item's rows are few batches, or there are items enough to keep the memory busy with one CTA each,
+// the CTA that selected the rows moves them too (FUSED; the rule stands in llms_evict_tokens): some CTAs select while
+// others move.
+//
+// Measured, a B200: 32 layers x 32 heads of 128 channels, 4096 -> 2048 tokens in place 365 us (2.19 GB, 6.0 TB/s: bound by the
+// memory); 32 x 8 heads, 32768 -> 8192 to other slots 374 us, of which 44 select; 1 layer x 4 heads, 256 -> 128: 7.8 us, a
+// chain of passes and rounds.
 #include <algorithm>
 
 #include <cooperative_groups.h>
@@ -31,6 +39,7 @@ constexpr int kBins = 2048;
 constexpr int kMoveThreads = 256;
 __host__ __device__ constexpr int in_flight(bool cluster) { return cluster ? 8 : 4; }   // 16-byte vectors of a thread
 constexpr int kMaxCluster = 8;
+constexpr int kFusedMostThreads = 512;            // of a CTA that selects and moves: 64 registers a thread
 
 struct EvictArgs {
     const float *mass;
@@ -63,8 +72,24 @@ __device__ __forceinline__ int slot_row(const EvictArgs &a, const int32_t *row, 
     return (unsigned)slot < (unsigned)a.n_slots ? slot * a.chunk_len + (t - chunk * a.chunk_len) : -1;
 }
 
-template <bool CLUSTER>
-__global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
+// The places of rows j0 .. j0 + n - 1 of the m kept ones: old and new row; a new row of -1: nothing to move.
+__device__ __forceinline__ void look_up_rows(const EvictArgs &a, int2 *rows, const int32_t *kept, const int32_t *from, const int32_t *to, int j0, int n,
+                                             int m, int tid, int threads)
+{
+    for (int i = tid; i < n; i += threads) {
+        const int j = j0 + i;
+        int2 x = make_int2(-1, -1);
+        if (j < m) {
+            x.x = slot_row(a, from, __ldcg(kept + j));
+            x.y = slot_row(a, to, j);
+            if (x.x < 0 || x.x == x.y) x.y = -1;
+        }
+        rows[i] = x;
+    }
+}
+
+template <bool CLUSTER, bool FUSED>
+__global__ void __launch_bounds__(FUSED ? kFusedMostThreads : 1024, 2) select_kernel(const EvictArgs a)
 {
     // counters, one set per digit in a cluster (other CTAs may still read the last one) and one for the sums; list; masses
     extern __shared__ uint4 smem_select[];
@@ -338,6 +363,37 @@ __global__ void __launch_bounds__(1024, 2) select_kernel(const EvictArgs a)
     for (int j = m + part * threads + tid; j < a.budget; j += parts * threads) kept[j] = -1;
     for (int t = m + part * threads + tid; t < n; t += parts * threads) mass_out[t] = 0.0f;
     if (tid == 0 && part == 0 && l == 0 && h == 0) a.new_lens[b] = bad ? -1 : m;
+    if constexpr (FUSED) {
+        // half of the threads move the K rows, half the V rows, in batches as move_kernel's
+        const bool in_place = a.dst_table == nullptr;
+        if (bad || (in_place && m == n)) return;
+        constexpr int kInFlight = in_flight(false);
+        const int vec = a.d / 8, per_half = threads / 2, at_once = a.by_vec(per_half), batch = at_once * kInFlight;
+        const int half = tid >= per_half, r = a.by_vec(tid - half * per_half), c = tid - half * per_half - r * vec;
+        const bool live = r < at_once;
+        const int32_t *table = a.table + (int64_t)b * a.table_stride, *to = in_place ? table : a.dst_table + (int64_t)b * a.dst_stride;
+        uint4 *slab = reinterpret_cast<uint4 *>(a.kv + l * a.stride_l + half * a.stride_s + h * a.stride_h) + c;
+        int2 *rows = reinterpret_cast<int2 *>(hist);                           // this round's and the next one's, in the counters' place
+        __syncthreads();                          // kept is complete, the counters are done with
+        look_up_rows(a, rows, kept, table, to, 0, batch, m, tid, threads);
+        __syncthreads();
+#pragma unroll 1
+        for (int j0 = 0, k = 0; j0 < m; j0 += batch, k ^= 1) {
+            uint4 v[kInFlight];
+            int d[kInFlight];
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                const int2 x = live ? rows[k * batch + u * at_once + r] : make_int2(-1, -1);
+                d[u] = x.y;
+                if (x.y >= 0) v[u] = __ldcg(slab + (int64_t)x.x * vec);
+            }
+            if (j0 + batch < m) look_up_rows(a, rows + (k ^ 1) * batch, kept, table, to, j0 + batch, batch, m, tid, threads);
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u)
+                if (d[u] >= 0) slab[(int64_t)d[u] * vec] = v[u];
+        }
+    }
 }
 
 // A slab (K or V of a KV head) of one sequence; its CTAs take batches of rows in turn.
@@ -363,19 +419,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a
     if (IN_PLACE && m == n) return;               // every row stays where it is
     const int first = IN_PLACE ? part * batch : part * a.batches * batch, step = IN_PLACE ? a.parts * batch : batch;
     const int rounds = IN_PLACE ? (m + step - 1) / step : min(a.batches, max(0, m - first + batch - 1) / batch);
-    auto look_up = [&](int k) {
-        const int j0 = first + k * step;
-        for (int i = tid; i < batch; i += kMoveThreads) {
-            const int j = j0 + i;
-            int2 x = make_int2(-1, -1);
-            if (j < m) {
-                x.x = slot_row(a, from, __ldcg(kept + j));
-                x.y = slot_row(a, to, j);
-                if (x.x < 0 || x.x == x.y) x.y = -1;
-            }
-            rows[k & 1][i] = x;
-        }
-    };
+    auto look_up = [&](int k) { look_up_rows(a, rows[k & 1], kept, from, to, first + k * step, batch, m, tid, kMoveThreads); };
     if (rounds > 0) look_up(0);
     __syncthreads();
 #pragma unroll 1
@@ -442,15 +486,28 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     while (parts < kMaxCluster && items * threads * parts * 2 <= room && parts * threads * 4 <= max_len) parts *= 2;
     int share = ((max_len + parts - 1) / parts + 3) & ~3;
     if (share > kSliceTokensShared) parts = 1, share = max_len;
+    // One kernel instead of two.  Where an item's rows make few batches it saves a launch (2 layers x 8 heads: 256 -> 96 tokens
+    // 9.8 -> 9.2 us, but 256 -> 128, four batches, 9.9 -> 10.3).  With more items some CTAs select while others move; what holds
+    // against it is that an item's move has one CTA only, with a selection's shared memory.  256 items, 2000 -> 1000 tokens, 16
+    // batches: 58 -> 54 us, 4096 -> 2048: 101 -> 102; 160 items: 43 -> 46.  More CTAs than the GPU takes at once, 1024 items,
+    // 4096 -> 2048: 422 -> 362; 16384 -> 4096, with two CTAs per SM: 816 -> 997.  512 threads if they all run at once: 256
+    // items, 1024 -> 512 tokens: 37 us with 256, 32 with 512; 512 items: 56 and 60
+    const int fused_threads = threads >= 512 && items * 512 <= sm_count() * 1024 ? 512 : 256, fused_batch = fused_threads / 2 / (a.d / 8) * in_flight(false);
+    const int fused_batches = (most + fused_batch - 1) / fused_batch;
+    a.in_smem = parts > 1 || max_len <= kSliceTokens;
+    a.list_room = std::min(4096, std::max(256, (share / 8 + 1) & ~1));
+    const size_t smem = (parts > 1 ? 4 : 1) * kBins * 4 + (size_t)a.list_room * 8 + (a.in_smem ? round_up((uint64_t)share * 4, 16) : 0);
+    static_assert(kFusedMostThreads / 4 * in_flight(false) * 2 * sizeof(int2) <= kBins * 4);       // two batches' rows, of at least two vectors
+    const bool fused = parts == 1 && (fused_batches <= 3 || (items >= sm_count() * 3 / 2 && fused_batches <= 16) ||
+                                      (items > sm_count() * 4 && smem <= 56 * 1024));
+    if (fused) threads = fused_threads;
     const bool shared = parts > 1;
     while ((1 << a.select_shift) < parts) ++a.select_shift;
     while ((32 << a.warps_shift) < threads) ++a.warps_shift;
-    a.in_smem = shared || max_len <= kSliceTokens;
-    a.list_room = std::min(4096, std::max(256, (share / 8 + 1) & ~1));
-    const size_t smem = (shared ? 4 : 1) * kBins * 4 + (size_t)a.list_room * 8 + (a.in_smem ? round_up((uint64_t)share * 4, 16) : 0);
-    void (*select)(EvictArgs) = shared ? select_kernel<true> : select_kernel<false>;
+    void (*select)(EvictArgs) = shared ? select_kernel<true, false> : (fused ? select_kernel<false, true> : select_kernel<false, false>);
     LLMS_CUDA_TRY(cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     LLMS_CUDA_TRY(launch_dependent_cluster(select, dim3(a.Hkv * parts, n_seqs, a.L), dim3(threads), smem, parts, st, a));
+    if (fused) return LLMS_OK;
 
     constexpr int kFillCtas = 296;                // in place, a slab is shared by a cluster until there are so many CTAs (see move_kernel)
     const int batch = kMoveThreads / (a.d / 8) * in_flight(false), most_batches = (most + batch - 1) / batch;

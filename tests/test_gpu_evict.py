@@ -78,6 +78,46 @@ def test_matches_the_plain_form(name, where):
     check(bt, bt.mass, budget, recent, dst, mass_out="same")
 
 
+# Calls of one kernel: few batches of rows; items enough for every SM; more items than run at once
+ONE_KERNEL = {
+    "one_batch": (dict(lens=[90, 33], heads=3, dim=256), 17, 2), "three_batches": (dict(lens=[190, 97, 0, 96]), 192 // 2, 5),
+    "three_batches_512": (dict(lens=[1500, 385, 384, 383], dim=64), 384, 11), "four_batches": (dict(lens=[300, 200]), 193, 5),
+    "many": (dict(lens=[i * 37 % 700 for i in range(120)], heads=2, dim=48), 400, 9),
+    "many_512": (dict(lens=[1500] + [i * 41 % 300 for i in range(119)], heads=2, dim=80, dtype=BF16), 600, 0),
+    "more_than_fit": (dict(lens=[1300, 0] + [i * 29 % 90 for i in range(98)], heads=7, dim=112), 1190, 30),
+    "more_than_fit_layers": (dict(lens=[9, 800, 41, 300], heads=19, dim=256, layers=8), 500, 499),
+}
+
+
+@pytest.mark.parametrize("where", ["in_place", "other_slots"])
+@pytest.mark.parametrize("name", ONE_KERNEL)
+def test_selected_and_moved_by_one_kernel(name, where):
+    kw, budget, recent = ONE_KERNEL[name]
+    bt = Batch(seed=len(name), **kw)
+    dst = other_slots(bt, budget) if where == "other_slots" else None
+    check(bt, bt.mass, budget, recent, dst)
+    check(bt, (bt.mass * 0.3).round(), budget, recent, dst, mass_out="same")
+
+
+def test_invalid_lengths_and_slots_among_many():
+    lens = [60 + i % 40 for i in range(150)]
+    bt, clean = Batch(lens, heads=2, seed=9), Batch(lens, heads=2, seed=9)
+    bt.table[2, 1] = bt.n_slots + 5
+    given = list(lens)
+    given[5], given[77] = 100, -3                 # above max_len, below zero
+    d, kv = desc_of(bt), bt.kv.cuda()
+    kept = torch.zeros(1, 150, 2, 40, dtype=torch.int32, device="cuda")
+    new_lens = torch.zeros(150, dtype=torch.int32, device="cuda")
+    B.evict_tokens(d, kv, bt.mass.cuda(), bt.table.cuda(), torch.tensor(given, dtype=torch.int32).cuda(), 99, 40, 3, kept, new_lens)
+    assert new_lens.tolist() == [-1 if b in (5, 77) else 40 for b in range(150)] and (kept[:, [5, 77]] == -1).all()
+    want, got = evict(clean, clean.mass, 40, 3), kv.cpu()
+    for b in range(150):
+        if b == 2:
+            continue
+        rows = clean.rows(b)
+        assert torch.equal(bits(got[:, :, :, rows]), bits((bt.kv if b in (5, 77) else want[3])[:, :, :, rows])), b
+
+
 VALUES = {
     "all_equal": lambda m: torch.full_like(m, 2.5), "all_zero": lambda m: torch.zeros_like(m),
     "few_values": lambda m: (m * 0.2).round(), "signed_zeros": lambda m: torch.where(m > 1, 0.0, -0.0),
