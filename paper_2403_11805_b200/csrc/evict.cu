@@ -34,7 +34,7 @@ namespace llms {
 namespace cg = cooperative_groups;
 
 constexpr int kSliceTokens = 16384;               // masses that a CTA holds in shared memory; of longer sequences it reads them again,
-constexpr int kSliceTokensShared = 49152;         // but a cluster's CTAs hold theirs
+constexpr int kSliceTokensShared = 40960;         // but a cluster's CTAs hold theirs (with four sets of counters and the longest list 224 KiB)
 constexpr int kBins = 2048;
 constexpr int kMoveThreads = 256;
 __host__ __device__ constexpr int in_flight(bool cluster) { return cluster ? 8 : 4; }   // 16-byte vectors of a thread
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(FUSED ? kFusedMostThreads : 1024, 2) select_ke
         const bool live = r < at_once;
         const int32_t *table = a.table + (int64_t)b * a.table_stride, *to = in_place ? table : a.dst_table + (int64_t)b * a.dst_stride;
         uint4 *slab = reinterpret_cast<uint4 *>(a.kv + l * a.stride_l + half * a.stride_s + h * a.stride_h) + c;
-        int2 *rows = reinterpret_cast<int2 *>(hist);                           // this round's and the next one's, in the counters' place
+        int2 *rows = reinterpret_cast<int2 *>(hist);                           // of these rows and of the next ones, in the counters' place
         __syncthreads();                          // kept is complete, the counters are done with
         look_up_rows(a, rows, kept, table, to, 0, batch, m, tid, threads);
         __syncthreads();

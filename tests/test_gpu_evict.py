@@ -118,6 +118,13 @@ def test_invalid_lengths_and_slots_among_many():
         assert torch.equal(bits(got[:, :, :, rows]), bits((bt.kv if b in (5, 77) else want[3])[:, :, :, rows])), b
 
 
+@pytest.mark.parametrize("tokens", [327680, 327681, 393216, 500001])
+def test_masses_up_to_and_beyond_a_cluster_s_shared_memory(tokens):
+    bt = Batch([tokens, 3], heads=1, dim=16, seed=2)
+    check(bt, bt.mass, 1000, 10)
+    check(bt, bt.mass, tokens // 3, 10, mass_out="same")
+
+
 VALUES = {
     "all_equal": lambda m: torch.full_like(m, 2.5), "all_zero": lambda m: torch.zeros_like(m),
     "few_values": lambda m: (m * 0.2).round(), "signed_zeros": lambda m: torch.where(m > 1, 0.0, -0.0),
