@@ -312,11 +312,21 @@ class MultiApp:
                 self._load(missing)
             self.table["last_access_step"][rows] = self.step_no
         self._ev_ready.record(self.main)                 # the working sets are resident: inference could start
-        if serve is not None:
-            batch = Serving(self, ctxs)
-            serve(batch)
-            batch.close()
-            locked_rows = np.concatenate([self.rows(c) for c in ctxs])
+        try:
+            if serve is not None:
+                batch = Serving(self, ctxs)
+                try:
+                    serve(batch)
+                finally:
+                    batch.close()                        # what it did to the contexts stands, also if it raised
+                    locked_rows = np.concatenate([self.rows(c) for c in ctxs])
+        finally:
+            self._leave(locked_rows)
+        self.ready_ms.append(self._ev_t0.elapsed_time(self._ev_ready))
+        return ctxs
+
+    def _leave(self, locked_rows):
+        """The end of a step: its working sets are unlocked, what was written back is settled."""
         self.clean[locked_rows] = False                  # a served context counts as modified by its call
         self.table["locked"][locked_rows] = 0
         self._end_of_step()                              # also settles the write-back left running by the step before
@@ -329,8 +339,6 @@ class MultiApp:
                 self._ev_aot = B.new_event(self.side_out)
             self._ev_aot.record(self.side_out)
             self._aot_rows = locked_rows
-        self.ready_ms.append(self._ev_t0.elapsed_time(self._ev_ready))
-        return ctxs
 
     def context_kv(self, c):
         """The resident KV of context c gathered from its slots, whole chunks: fp16 [L, 2, H, T, d] (device)."""

@@ -121,3 +121,26 @@ def test_serving_keeps_to_its_capacity():
     for _ in range(4):
         app.step(k=2)
         consistent(app)
+
+
+@pytest.mark.parametrize("aot", [False, True], ids=["reclaim", "aot"])
+def test_a_serve_that_raises_leaves_the_pool_in_order(aot):
+    sh = synth.KVShape("apps", 1, 2, 2, 64, 64, 16, 64, window=4, seed=1, n_contexts=4)
+    app = MultiApp(sh, n_slots=8, seed=3, aot=aot)
+    app.build()
+    served = []
+
+    def serve(s):
+        served.extend(s.ctxs)
+        s.shrink(20, 4)
+        s.advance()
+        raise KeyError("the model's own")
+
+    with pytest.raises(KeyError):
+        app.step(k=2, serve=serve)
+    consistent(app)
+    assert len(served) == 2 and [app.lengths[c] for c in served] == [21, 21] and not app.table["locked"].any()
+    for _ in range(4):
+        app.step(k=2)
+        consistent(app)
+    app.finish()
