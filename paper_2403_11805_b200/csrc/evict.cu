@@ -8,6 +8,7 @@
 // sign, exponent and two bits of the fraction, so that masses that differ by powers of two - attention weights do - spread
 // over the counters, and few are left with the limit's first digit: these are listed in the pass that counts the kept
 // tokens, and the other digits are found from the list.  The masses stay in shared memory for the passes if they fit.
+// Of few tokens, one per thread, each is compared with every other instead.
 //
 // Rows (move_kernel).  A kept row is read and written once, 8 * head_dim bytes for K and V together: memory-bound, in pieces of a row
 // (2 * head_dim bytes) at scattered places.  Whole rows are moved by neighbouring lanes, rows in the order of their
@@ -20,9 +21,9 @@
 // the CTA that selected the rows moves them too (FUSED; the rule stands in llms_evict_tokens): some CTAs select while
 // others move.
 //
-// Measured, a B200: 32 layers x 32 heads of 128 channels, 4096 -> 2048 tokens in place 365 us (2.19 GB, 6.0 TB/s: bound by the
-// memory); 32 x 8 heads, 32768 -> 8192 to other slots 374 us, of which 44 select; 1 layer x 4 heads, 256 -> 128: 7.8 us, a
-// chain of passes and rounds.
+// Measured, a B200: 32 layers x 32 heads of 128 channels, 4096 -> 2048 tokens in place 364 us (2.19 GB, 6.0 TB/s: bound by the
+// memory); 32 x 8 heads, 32768 -> 8192 to other slots 374 us, of which 44 select; 1 layer x 4 heads, 256 -> 128: 6.4 us, a
+// chain of comparisons and rounds.
 #include <algorithm>
 
 #include <cooperative_groups.h>
@@ -39,6 +40,9 @@ constexpr int kBins = 2048;
 constexpr int kMoveThreads = 256;
 __host__ __device__ constexpr int in_flight(bool cluster) { return cluster ? 8 : 4; }   // 16-byte vectors of a thread
 constexpr int kMaxCluster = 8;
+// Up to so many tokens each candidate is compared with every other: 4 items, 256 -> 16 tokens 6.8 us by digits, 5.8; 88 -> 3 tokens
+// 6.6 and 4.1
+constexpr int kPairTokens = 256;
 constexpr int kFusedMostThreads = 512;            // of a CTA that selects and moves: 64 registers a thread
 
 struct EvictArgs {
@@ -105,7 +109,9 @@ __global__ void __launch_bounds__(FUSED ? kFusedMostThreads : 1024, 2) select_ke
     const float *mass = a.mass + row * a.mass_stride;
     float *mass_out = a.mass_out + row * a.mass_stride;
     int32_t *kept = a.kept + row * a.budget;
-    for (int i = tid; i < (CLUSTER ? 3 : 1) * kBins / 4; i += threads) smem_select[i] = make_uint4(0, 0, 0, 0);
+    const bool no_digits = !CLUSTER && a.max_len <= min(threads, kPairTokens);
+    if (!no_digits)
+        for (int i = tid; i < (CLUSTER ? 3 : 1) * kBins / 4; i += threads) smem_select[i] = make_uint4(0, 0, 0, 0);
     grid_dependency_wait();
     grid_launch_dependents();
     const int len = __ldg(a.lens + b);
@@ -115,7 +121,8 @@ __global__ void __launch_bounds__(FUSED ? kFusedMostThreads : 1024, 2) select_ke
     const int share = CLUSTER ? (((n + parts - 1) >> a.select_shift) + 3) & ~3 : n, t0 = CLUSTER ? min(n, part * share) : 0, count = min(n, t0 + share) - t0;
     // (none if they all stay).  Values above the limit's stay, and the first `need` ones equal to it
     const int mine = quota >= cand ? 0 : max(0, min(count, cand - t0));
-    const bool ranked = quota > 0 && quota < cand;
+    const bool pairs = !CLUSTER && a.in_smem && n <= min(threads, kPairTokens);
+    const bool ranked = quota > 0 && quota < cand && !pairs;
     uint32_t limit = 0, need = ranked ? quota : 0;
     const float *from = a.in_smem ? slice : mass;
     // four neighbouring masses (what lies behind the last one is -inf and counts nowhere)
@@ -237,7 +244,36 @@ __global__ void __launch_bounds__(FUSED ? kFusedMostThreads : 1024, 2) select_ke
         gt = i >= mine || v > border;
         eq = !gt && v == border;
     };
-    if (CLUSTER || a.in_smem || a.mass != a.mass_out) {
+    if (pairs) {
+        // a token per thread: it stays if fewer than `quota` candidates come before it.  Those of the warps before come before it
+        // if they are as heavy, those of the warps behind if they are heavier
+        const float w = tid < n ? slice[tid] : 0.0f, v = fmaxf(w, -INFINITY);
+        const int own = warp * 32;
+        int before = 0;
+        bool stay = tid < n;
+        if (quota < cand && own < cand) {
+#pragma unroll 2
+            for (int j = 0; j < own; j += 4) {
+                const float4 x = *reinterpret_cast<const float4 *>(slice + j);
+                before += (fmaxf(x.x, -INFINITY) >= v) + (fmaxf(x.y, -INFINITY) >= v) + (fmaxf(x.z, -INFINITY) >= v) + (fmaxf(x.w, -INFINITY) >= v);
+            }
+#pragma unroll 8
+            for (int j = 0; j < 32; ++j) {
+                const float x = __shfl_sync(0xffffffffu, v, j);
+                before += own + j < cand && (j < lane ? x >= v : x > v);
+            }
+            for (int j = own + 32; j < cand; ++j) before += fmaxf(slice[j], -INFINITY) > v;
+            stay = stay && (tid >= cand || before < quota);
+        }
+        const uint32_t ballot = __ballot_sync(0xffffffffu, stay);
+        if (lane == 0) warp_sum[warp] = __popc(ballot);
+        __syncthreads();
+        const int to = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane] : 0u) + __popc(ballot & ((1u << lane) - 1u));
+        if (stay) {
+            kept[to] = tid;
+            mass_out[to] = w;
+        }
+    } else if (CLUSTER || a.in_smem || a.mass != a.mass_out) {
         // a warp takes neighbouring tokens, 32 at a time: it counts its ones, then numbers them in the order of positions
         if (listed) {
             for (int i = tid; i < (int)s_listed; i += threads) {
@@ -491,8 +527,13 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     // against it is that an item's move has one CTA only, with a selection's shared memory.  256 items, 2000 -> 1000 tokens, 16
     // batches: 58 -> 54 us, 4096 -> 2048: 101 -> 102; 160 items: 43 -> 46.  More CTAs than the GPU takes at once, 1024 items,
     // 4096 -> 2048: 422 -> 362; 16384 -> 4096, with two CTAs per SM: 816 -> 997.  512 threads if they all run at once: 256
-    // items, 1024 -> 512 tokens: 37 us with 256, 32 with 512; 512 items: 56 and 60
-    const int fused_threads = threads >= 512 && items * 512 <= sm_count() * 1024 ? 512 : 256, fused_batch = fused_threads / 2 / (a.d / 8) * in_flight(false);
+    // items, 1024 -> 512 tokens: 37 us with 256, 32 with 512; 512 items: 56 and 60.  128 for more than run at
+    // once and little to keep: 3024 items, 600 -> 100 tokens 88 us with 256, 84 with 128; 256 -> 16: 54 and 36; 600 -> 250: 151 and
+    // 148, but 2048 ragged ones of up to 1024 -> 512 tokens 58 and 62.  64 threads: 3024 items, 32 -> 8: 12.6 us with 128, 9.9 with 64
+    const int resident = sm_count() * 1024;       // threads
+    int fused_threads = threads >= 512 && items * 512 <= resident ? 512 : 256;
+    if (items * 256 > resident && most <= 256) fused_threads = max_len <= 64 ? 64 : 128;
+    const int fused_batch = fused_threads / 2 / (a.d / 8) * in_flight(false);
     const int fused_batches = (most + fused_batch - 1) / fused_batch;
     a.in_smem = parts > 1 || max_len <= kSliceTokens;
     a.list_room = std::min(4096, std::max(256, (share / 8 + 1) & ~1));

@@ -85,6 +85,10 @@ ONE_KERNEL = {
     "many": (dict(lens=[i * 37 % 700 for i in range(120)], heads=2, dim=48), 400, 9),
     "many_512": (dict(lens=[1500] + [i * 41 % 300 for i in range(119)], heads=2, dim=80, dtype=BF16), 600, 0),
     "more_than_fit": (dict(lens=[1300, 0] + [i * 29 % 90 for i in range(98)], heads=7, dim=112), 1190, 30),
+    "pairs": (dict(lens=[256, 255, 31, 32, 33, 0, 1, 2, 64], heads=3), 40, 7), "pairs_to_257": (dict(lens=[257, 256, 128]), 64, 0),
+    "short_many": (dict(lens=[i % 64 for i in range(1, 101)], heads=7, dim=256), 9, 2),
+    "pairs_many": (dict(lens=[i * 5 % 129 for i in range(100)], heads=7, dim=240, chunk=5), 70, 1),
+    "little_kept": (dict(lens=[i * 53 % 601 for i in range(100)], heads=7, dim=80, dtype=BF16), 256, 200),
     "more_than_fit_layers": (dict(lens=[9, 800, 41, 300], heads=19, dim=256, layers=8), 500, 499),
 }
 
@@ -143,6 +147,15 @@ def test_values(name):
     mass = VALUES[name](bt.mass)
     for budget, recent in ((100, 10), (299, 0), (41, 41)):
         check(bt, mass, budget, recent)
+
+
+@pytest.mark.parametrize("name", VALUES)
+def test_values_of_few_tokens(name):
+    bt = Batch([250, 41, 0, 97, 33], layers=2, seed=4)
+    mass = VALUES[name](bt.mass)
+    for budget, recent in ((100, 10), (32, 0), (41, 41), (249, 0), (1, 0)):
+        check(bt, mass, budget, recent)
+        check(bt, mass, budget, recent, mass_out="same")
 
 
 def test_dst_table_may_be_the_table_itself():
