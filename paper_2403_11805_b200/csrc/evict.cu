@@ -437,7 +437,7 @@ template <bool IN_PLACE, bool CLUSTER>
 __global__ void __launch_bounds__(kMoveThreads, 4) move_kernel(const EvictArgs a)
 {
     constexpr int kInFlight = in_flight(CLUSTER), kMostRows = kMoveThreads / 2 * kInFlight;                   // of a batch: rows have at least two vectors
-    __shared__ int2 rows[2][kMostRows];           // old and new row, of this round and the next; a new row of -1: nothing to move
+    __shared__ int2 rows[2][kMostRows];           // old and new row, of this batch and the next; a new row of -1: nothing to move
     const int vec = a.d / 8, at_once = a.by_vec(kMoveThreads), batch = at_once * kInFlight, tid = threadIdx.x;
     const int r = a.by_vec(tid), c = tid - r * vec;
     const bool live = r < at_once;
