@@ -328,8 +328,8 @@ int llms_decode_attention(const llms_kv_desc *desc, int dtype, int layer, void *
  *   budget    >= 1;  recent  0 .. budget
  *   dst_table device int32 [n_seqs][dst_stride], dst_stride * chunk_len >= min(budget, max_len): where positions 0 .. m-1
  *             go.  Every slot listed there (for those positions) must be one that this call does not read, and listed once.
- *             NULL, or chunk_table itself: the rows stay in the sequence's own chunks (in place; then a slot must not be
- *             listed by two sequences)
+ *             NULL, or chunk_table's own address (with several sequences its stride too, LLMS_ERR_INVALID_ARG otherwise):
+ *             the rows stay in the sequence's own chunks (in place; then a slot must not be listed twice)
  *   mass_out  like mass, may be the same array but not overlap it otherwise: masses of positions 0 .. m-1, then zeros up to
  *             lens[b]; entries from lens[b] on are left as they were
  *   kept      device int32 [n_layers][n_seqs][n_kv_heads][budget]: the kept positions, ascending, then -1

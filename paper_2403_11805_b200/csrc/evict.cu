@@ -492,9 +492,12 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     if (n_seqs == 0) return LLMS_OK;
     if (!kv || !mass || !chunk_table || !lens || !mass_out || !kept || !new_lens || new_lens == lens) return LLMS_ERR_INVALID_ARG;
     if (table_stride < 1 || (int64_t)table_stride * desc->chunk_len < max_len || mass_stride < max_len) return LLMS_ERR_INVALID_ARG;
-    if (dst_table == chunk_table && dst_stride == table_stride) dst_table = nullptr;   // the sequence's own chunks
     const int most = budget < max_len ? budget : max_len;
     if (dst_table && (dst_stride < 1 || (int64_t)dst_stride * desc->chunk_len < most)) return LLMS_ERR_INVALID_ARG;
+    if (dst_table == chunk_table) {               // the sequences' own chunks; of one sequence the strides mean nothing
+        if (n_seqs > 1 && dst_stride != table_stride) return LLMS_ERR_INVALID_ARG;
+        dst_table = nullptr;
+    }
     if (!aligned(kv, 16)) return LLMS_ERR_MISALIGNED;
     if (!aligned(mass, 4) || !aligned(mass_out, 4) || !aligned(chunk_table, 4) || !aligned(lens, 4) || !aligned(dst_table, 4) ||
         !aligned(kept, 4) || !aligned(new_lens, 4))

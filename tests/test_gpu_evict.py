@@ -175,6 +175,22 @@ def test_the_table_as_its_own_destination_is_in_place():
     assert torch.equal(kept.cpu(), want[0]) and torch.equal(bits(kv.cpu()), bits(want[3]))
 
 
+@pytest.mark.parametrize("lens", [[2000], [2000, 1500, 700]], ids=["one", "several"])
+@pytest.mark.parametrize("view", ["whole", "first_chunks"])
+def test_a_view_of_the_table_as_destination_is_in_place(view, lens):
+    """16 batches of rows and a kernel of their own for moving: rows taken in another order than upwards would be overwritten."""
+    bt = Batch(lens, heads=4, dim=128, seed=15)
+    dev, n_lens = bt.table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+    dst = dev if view == "whole" else dev[:, :-(-1000 // bt.chunk)]
+    n = len(lens)
+    kept, new_lens = torch.zeros(1, n, 4, 1000, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    kv, mass = bt.kv.cuda(), bt.mass.cuda()
+    B.evict_tokens(desc_of(bt), kv, mass, dev, n_lens, 2000, 1000, 40, kept, new_lens, dst_table=dst)
+    want = evict(bt, bt.mass, 1000, 40, None, bt.mass)
+    assert torch.equal(kept.cpu(), want[0]) and torch.equal(new_lens.cpu(), want[1])
+    assert torch.equal(mass.cpu(), want[2]) and torch.equal(bits(kv.cpu()), bits(want[3]))
+
+
 def test_in_place_twice_and_repeatable():
     bt = Batch([3000, 777], heads=4, dim=128, seed=6, layers=2)
     first = call(bt, bt.mass, 1500, 64)

@@ -82,6 +82,12 @@ def test_evict_refusals(status, kw):
     assert evict(**kw) == status
 
 
+def test_a_table_as_its_own_destination_keeps_its_stride():
+    """With several sequences another stride would make rows of one the places of another."""
+    assert evict(dst_table=A, table_stride=8, dst_stride=5) == INVALID
+    assert evict(dst_table=A, table_stride=5, dst_stride=8) == INVALID
+
+
 def test_an_empty_batch_does_nothing():
     assert decode(n_seqs=0, q=None, out=None) == B.OK
     assert evict(n_seqs=0, kept=None) == B.OK
