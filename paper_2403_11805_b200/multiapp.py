@@ -71,8 +71,7 @@ class MultiApp:
             kvs.append(kv.cpu() if self.keep_sources else None)
             self._place_in_arena(c, bits)
             self._first_compress(c, kv, bits)
-        torch.cuda.synchronize()
-        self._collect_checksums()
+        self._settle()
         self.sources = kvs
         self.bits = all_bits
         resident = self.n_slots // self.cpc
@@ -103,7 +102,9 @@ class MultiApp:
         self.ws = [torch.empty(B.codec_workspace_bytes(self.cpc), dtype=torch.uint8, device="cuda") for _ in range(64)]
         self.metas = [B.new_meta(self.cpc, pinned=True) for _ in range(64)]
         self._ws_next = 0
+        self._ws_taken = 0                        # entries of the ring that hold results nobody has read yet, at most
         self._used_ws = []
+        self._corrupt = 0                         # records that failed their checksum, not reported yet
         self.ev_stage_out_free = [B.new_event() for _ in range(n_out)]
         self.ev_stage_in_free = [B.new_event() for _ in range(2)]
         self.ev_compressed = [B.new_event() for _ in range(n_out)]
@@ -115,6 +116,11 @@ class MultiApp:
         self.arena = torch.empty(total, dtype=torch.uint8).pin_memory()
 
     def _next_ws(self):
+        """A workspace and a meta array for a codec call.  They are a ring: once all have been taken, their results (a compress
+        call's checksums, a decompress call's count of corrupt records) are read before the first is used again."""
+        if self._ws_taken == len(self.ws):
+            self._settle()
+        self._ws_taken += 1
         i = self._ws_next % len(self.ws)
         self._ws_next += 1
         return self.ws[i], self.metas[i]
@@ -131,9 +137,6 @@ class MultiApp:
         B.swap_out(self.stage_out[k], meta, self.arena, host_offsets=self.arena_off[rows], side_stream=self.side_out,
                    after=self.ev_compressed[k], done=self.ev_stage_out_free[k], n=len(rows))
         self._pending.append((meta, rows))
-        if len(self._pending) >= len(self.ws) - 2:
-            torch.cuda.synchronize()
-            self._collect_checksums()
 
     def _collect_checksums(self):
         for meta, rows in self._pending:
@@ -190,11 +193,18 @@ class MultiApp:
             self._collect_checksums()
             self._aot_rows = None
 
-    def finish(self):
-        """Everything queued has completed and every checksum is known on the host."""
+    def _settle(self):
+        """Everything queued completes, and the results of the codec calls are taken."""
         torch.cuda.synchronize()
         self._collect_checksums()
+        self._corrupt += sum(B.codec_corrupt_count(ws) for ws in self._used_ws)
+        self._used_ws = []
+        self._ws_taken = 0
         self._aot_rows = None
+
+    def finish(self):
+        """Everything queued has completed and every checksum is known on the host."""
+        self._settle()
 
     def _load(self, rows):
         """Load: copy the records of the chunks in `rows` from the arena, unpack + dequantize into free slots."""
@@ -237,10 +247,8 @@ class MultiApp:
 
     def _end_of_step(self):
         """One synchronisation per step: read back the checksums of this step's records, check the decoded ones."""
-        torch.cuda.synchronize()
-        self._collect_checksums()
-        bad = sum(B.codec_corrupt_count(ws) for ws in self._used_ws)
-        self._used_ws = []
+        self._settle()
+        bad, self._corrupt = self._corrupt, 0
         if bad:
             raise RuntimeError(f"{bad} records failed their checksum on the way in")
 
@@ -330,7 +338,6 @@ class MultiApp:
         self.clean[locked_rows] = False                  # a served context counts as modified by its call
         self.table["locked"][locked_rows] = 0
         self._end_of_step()                              # also settles the write-back left running by the step before
-        self._aot_rows = None
         if self.aot:
             # ahead-of-time swap-out when the call returns (Sec. 3.4 i): queued now, left running, so that its
             # copies out share the link with the next step's copies in

@@ -144,3 +144,49 @@ def test_a_serve_that_raises_leaves_the_pool_in_order(aot):
         app.step(k=2)
         consistent(app)
     app.finish()
+
+
+def test_more_reclaims_in_a_step_than_the_pool_has_workspaces():
+    """A context grows by 90 chunks in one call while the pool is full of modified ones: each growth reclaims a chunk of others, and
+    every record that left has its own checksum and comes back."""
+    sh = synth.KVShape("apps", 1, 1, 1, 64, 100 * 16, 16, 64, window=4, seed=4, n_contexts=4)         # 100 chunks per context
+    app = MultiApp(sh, n_slots=200, seed=2)
+    app.build()
+    chosen = []
+    app.draw_contexts = lambda k: list(chosen)
+
+    def step(c, serve=None):
+        chosen[:] = [c]
+        app.step(k=1, serve=serve)
+        consistent(app)
+
+    step(2, lambda s: s.shrink(16, 1))
+    step(3)
+    step(1)
+    full = app.pool.cpu()
+    slots = {r: int(app.slot[r]) for r in np.flatnonzero(app.slot >= 0)}
+    app.clean[list(slots)] = False
+    one = odesc(sh.with_(n_tokens=16))
+
+    def grow(s):
+        for _ in range(90 * 16):
+            s.advance()
+
+    before = app._ws_next
+    step(2, grow)
+    assert app._ws_next - before > 64
+    gone = [r for r in slots if app.slot[r] < 0]
+    assert len(gone) >= 80
+    records = {}
+    for r in gone:
+        chunk = np.ascontiguousarray(bits_view(full[..., slots[r] * 16:(slots[r] + 1) * 16, :]))
+        buf, meta = oracle.compress_chunks(one, chunk, [0], [int(app.table["bits"][r])])
+        assert app.checksum[r] == meta[0]["checksum"], r
+        out = np.zeros_like(chunk)
+        oracle.decompress_chunks(one, buf, meta, out)
+        records[r] = out
+    for c in (1, 3):
+        step(c)
+        for i, r in enumerate(app.rows(c)):
+            if r in records:
+                assert np.array_equal(bits_view(app.context_kv(c))[..., i * 16:(i + 1) * 16, :], records[r])

@@ -1,0 +1,199 @@
+"""The multi-app pool's bookkeeping without a GPU: the module itself, over a device that is imitated on the host.
+
+Work that the module queues runs when the host waits for it and not before, in the order in which it was queued, as on a device
+that is always behind: meta arrays and workspaces hold results only then.  A chunk's content is one number, which is its record
+and its checksum too."""
+import types
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2403_11805_b200 import binding as B, multiapp, serving, synth
+
+
+class Device:
+    """Slots, the swap buffers' and the arena's records by position, and the work queued for them."""
+
+    def __init__(self):
+        self.queue, self.slots, self.staged, self.arena, self.corrupt, self.fresh = [], {}, {}, {}, {}, 1000
+        self.waits = 0
+
+    def wait(self, *_):
+        self.waits += 1
+        for work in self.queue:
+            work()
+        self.queue = []
+
+    def new_content(self):
+        self.fresh += 1
+        return self.fresh
+
+    # ---- the binding's calls
+    def compress_chunks(self, desc, kv, ids, bits, out, meta, ws, **_):
+        ids = [int(i) for i in ids]
+
+        def work():
+            for i, slot in enumerate(ids):
+                meta["checksum"][i] = self.slots[slot]
+            self.staged[out.data_ptr()] = [self.slots[slot] for slot in ids]
+            self.corrupt[ws.data_ptr()] = 0                  # a call's workspace begins as zeros
+        self.queue.append(work)
+
+    def swap_out(self, buf, meta, arena, host_offsets, n, **_):
+        where = [int(x) for x in host_offsets]
+        self.queue.append(lambda: self.arena.update(zip(where, self.staged[buf.data_ptr()])))
+
+    def swap_in(self, arena, meta, buf, host_offsets, **_):
+        where = [int(x) for x in host_offsets]
+        self.queue.append(lambda: self.staged.update({buf.data_ptr(): [self.arena[x] for x in where]}))
+
+    def decompress_chunks(self, desc, buf, meta, ids, kv, ws):
+        slots, sums = [int(x) for x in meta["chunk_id"]], [int(x) for x in meta["checksum"]]   # read when the call is made
+
+        def work():
+            got = self.staged[buf.data_ptr()]
+            self.corrupt[ws.data_ptr()] = sum(a != b for a, b in zip(got, sums))
+            self.slots.update(zip(slots, got))
+        self.queue.append(work)
+
+    def codec_corrupt_count(self, ws):
+        self.wait()
+        return self.corrupt[ws.data_ptr()]
+
+    def evict_tokens(self, desc, kv, mass, table, lens, max_len, budget, recent, kept, new_lens, **_):
+        new_lens.copy_(lens.clamp(max=budget))
+
+
+class Event:
+    def __init__(self, device):
+        self.synchronize = device.wait
+
+    def record(self, *_):
+        pass
+
+    def elapsed_time(self, other):
+        return 0.0
+
+
+class Stream:
+    cuda_stream = 0
+
+    def wait_event(self, *_):
+        pass
+
+    wait_stream = wait_event
+
+
+@pytest.fixture
+def device(monkeypatch):
+    dev = Device()
+
+    def made(name):
+        def make(*shape, device=None, **kw):
+            return getattr(torch, name)(*shape, **kw)
+        return make
+
+    stream = Stream()
+    cuda = types.SimpleNamespace(synchronize=dev.wait, current_stream=lambda *_: stream, Stream=Stream, Event=lambda **_: Event(dev))
+    fake = types.SimpleNamespace(cuda=cuda, **{n: made(n) for n in ("zeros", "empty", "full")},
+                                 **{n: getattr(torch, n) for n in ("from_numpy", "empty_like", "cat", "uint8", "int32", "float16", "float32")})
+    monkeypatch.setattr(multiapp, "torch", fake)
+    monkeypatch.setattr(serving, "torch", fake)
+    monkeypatch.setattr(torch.Tensor, "cuda", lambda self, *_, **__: self.clone())
+    monkeypatch.setattr(torch.Tensor, "pin_memory", lambda self, *_, **__: self)
+    for name in ("compress_chunks", "swap_out", "swap_in", "decompress_chunks", "codec_corrupt_count", "evict_tokens"):
+        monkeypatch.setattr(B, name, getattr(dev, name))
+    monkeypatch.setattr(B, "new_event", lambda *_: Event(dev))
+    return dev
+
+
+CHUNKS = 100
+
+
+def pool(device, n_contexts=4, aot=False):
+    """Contexts of 100 chunks of 16 tokens with room for two of them; every record in the arena, the first two contexts resident
+    and modified since."""
+    sh = synth.KVShape("apps", 1, 1, 1, 16, CHUNKS * 16, 16, 16, window=4, seed=1, n_contexts=n_contexts)
+    app = multiapp.MultiApp(sh, n_slots=2 * CHUNKS, seed=1, aot=aot)
+    app._alloc_buffers()
+    for c in range(n_contexts):
+        bits, _ = B.assign_bits(np.arange(CHUNKS, dtype=np.float32), app.frac)
+        app._place_in_arena(c, bits)
+    for row in range(n_contexts * CHUNKS):
+        app.checksum[row] = device.arena[int(app.arena_off[row])] = device.new_content()
+    for c in range(2):
+        app._load(np.arange(c * CHUNKS, (c + 1) * CHUNKS))
+    app._end_of_step()
+    modify(device, app, range(2 * CHUNKS))
+    app.chosen = []
+    app.draw_contexts = lambda k: app.chosen
+    return app
+
+
+def modify(device, app, rows):
+    """The chunks in these rows get other content, behind everything that is queued."""
+    slots = [int(app.slot[r]) for r in rows]
+    device.queue.append(lambda: device.slots.update((s, device.new_content()) for s in slots))
+    app.clean[rows] = False
+
+
+def step(app, ctxs, serve=None):
+    app.chosen = list(ctxs)
+    return app.step(k=len(ctxs), serve=serve)
+
+
+def grow(device, app, chunks):
+    """A serve callback: every context of the batch grows by so many chunks."""
+    def serve(s):
+        for _ in range(chunks):
+            for _ in range(16):
+                s.advance()
+            for i, c in enumerate(s.ctxs):
+                modify(device, app, [c * CHUNKS + (int(s.lengths[i]) - 1) // 16])
+    return serve
+
+
+def crowded(device):
+    """Context 2 is down to one chunk and out; the pool is full of modified chunks of contexts 1 and 3, and their content by row."""
+    app = pool(device)
+    step(app, [2], lambda s: s.shrink(16, 1))
+    step(app, [3])
+    step(app, [1])
+    if app.slot[2 * CHUNKS] >= 0:
+        app._evict([2 * CHUNKS])
+    rows = np.flatnonzero(app.slot >= 0)
+    modify(device, app, rows)
+    app._end_of_step()
+    return app, {int(r): device.slots[int(app.slot[r])] for r in rows}
+
+
+def test_more_reclaims_in_a_step_than_the_ring_has_entries(device):
+    app, was = crowded(device)
+    before = app._ws_next
+    step(app, [2], grow(device, app, 95))
+    assert app._ws_next - before > len(app.ws) + 20
+    gone = [r for r in was if app.slot[r] < 0]
+    assert len(gone) >= 90
+    wrong = [r for r in gone if app.checksum[r] != was[r]]
+    assert not wrong, f"{len(wrong)} of {len(gone)} records have another record's checksum"
+    assert all(device.arena[int(app.arena_off[r])] == was[r] for r in gone)
+    step(app, [1])                                           # and they are read back
+    step(app, [3])
+    back = [r for r in gone if app.slot[r] >= 0]
+    assert back and all(device.slots[int(app.slot[r])] == was[r] for r in back)
+
+
+def test_a_corrupt_record_is_reported_however_much_follows_in_its_step(device):
+    app, _ = crowded(device)
+    device.arena[int(app.arena_off[2 * CHUNKS])] += 1
+    with pytest.raises(RuntimeError, match="checksum"):
+        step(app, [2], grow(device, app, 95))
+    step(app, [1])                                           # reported once
+
+
+def test_a_step_of_few_reclaims_waits_at_its_end_only(device):
+    app, _ = crowded(device)
+    waits, inside = device.waits, []
+    step(app, [2], lambda s: (grow(device, app, 40)(s), inside.append(device.waits - waits)))
+    assert inside == [0]
