@@ -1042,9 +1042,9 @@ static bool encode_layer(CUtensorMap *map, const void *base, bool bf16, const ll
     const cuuint64_t dims[5] = {whole ? 64 : (cuuint64_t)d.head_dim, (cuuint64_t)d.n_tokens, n_blocks, (cuuint64_t)d.n_kv_heads, 2};
     const cuuint64_t strides[4] = {(cuuint64_t)d.head_dim * 2, 128, head * 2, (cuuint64_t)d.stride_s * 2};
     const cuuint32_t box[5] = {64, (cuuint32_t)piece, n_blocks, 1, whole ? 2u : 1u}, elem[5] = {1, 1, 1, 1, 1};
-    return tensor_map_encoder()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, const_cast<void *>(base),
-                                dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode_tensor_map(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, const_cast<void *>(base), dims,
+                             strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
 template <bool BF, int DB, int MODE>
@@ -1134,7 +1134,6 @@ extern "C" int llms_decode_attention(const llms_kv_desc *desc, int dtype, int la
     if (!aligned(chunk_table, 4) || !aligned(lens, 4) || !aligned(lse, 4) || !aligned(mass_in, 4) || !aligned(mass_out, 4)) return LLMS_ERR_MISALIGNED;
     const DecodeLayout lay = decode_layout(*desc, n_seqs, max_len, mass_out != nullptr);
     if (workspace_bytes < lay.total) return LLMS_ERR_BUF_TOO_SMALL;
-    if (!tensor_map_encoder()) return LLMS_ERR_UNSUPPORTED;
 
     DecodeArgs a{};
     a.q = static_cast<const uint16_t *>(q);

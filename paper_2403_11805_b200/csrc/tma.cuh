@@ -26,6 +26,18 @@ inline EncodeTiledFn tensor_map_encoder()
     return fn;
 }
 
+// The encoder's call; false if there is none or it refuses.  It wants a current context, which a host thread has from its first
+// use of the device through the runtime on: a thread that has none yet gets it here.
+template <typename... Args>
+inline bool encode_tensor_map(Args... args)
+{
+    const EncodeTiledFn encode = tensor_map_encoder();
+    if (!encode) return false;
+    if (encode(args...) == CUDA_SUCCESS) return true;
+    int device = 0;
+    return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess && encode(args...) == CUDA_SUCCESS;
+}
+
 // ---- device
 
 constexpr uint32_t kSpinLimit = 1u << 22;            // polls (with a pause in between) before a wait is given up

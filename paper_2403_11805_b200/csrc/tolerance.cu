@@ -807,8 +807,6 @@ static int launch_logits_tc_rows(const TolArgs &a, int R, const CUtensorMap &map
 
 static int launch_logits_tc(const TolArgs &a, int SEG, cudaStream_t st)
 {
-    EncodeTiledFn encode = tensor_map_encoder();
-    if (!encode) return LLMS_ERR_UNSUPPORTED;
     const int R = tc_rows(a);
     // K as a 4-D tensor (channel, token, KV head, layer), tiles of 64 channels x 128 tokens, 128-byte swizzle; tokens past
     // the end of the context read as zeros
@@ -817,18 +815,18 @@ static int launch_logits_tc(const TolArgs &a, int SEG, cudaStream_t st)
         const cuuint64_t dims[4] = {(cuuint64_t)a.d, (cuuint64_t)a.T, (cuuint64_t)a.Hkv, (cuuint64_t)a.L};
         const cuuint64_t strides[3] = {(cuuint64_t)a.d * 2, (cuuint64_t)a.stride_h * 2, (cuuint64_t)a.stride_l * 2};
         const cuuint32_t box[4] = {64, (cuuint32_t)kTcWide, 1, 1}, elem[4] = {1, 1, 1, 1};
-        if (encode(&map_k, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<__half *>(a.kv), dims, strides, box, elem,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        if (!encode_tensor_map(&map_k, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<__half *>(a.kv), dims, strides, box, elem,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE))
             return LLMS_ERR_UNSUPPORTED;
     }
     {   // the query window as a matrix of (layer, head, row) x channel, R rows at a time
         const cuuint64_t dims[2] = {(cuuint64_t)a.d, (cuuint64_t)a.L * a.Hq * a.W};
         const cuuint64_t strides[1] = {(cuuint64_t)a.d * 2};
         const cuuint32_t box[2] = {64, (cuuint32_t)R}, elem[2] = {1, 1};
-        if (encode(&map_q, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half *>(a.q_win), dims, strides, box, elem,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        if (!encode_tensor_map(&map_q, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half *>(a.q_win), dims, strides, box, elem,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE))
             return LLMS_ERR_UNSUPPORTED;
     }
     if (SEG == 16) return a.d == 64 ? launch_logits_tc_rows<16, 64>(a, R, map_k, map_q, st) : launch_logits_tc_rows<16, 128>(a, R, map_k, map_q, st);
