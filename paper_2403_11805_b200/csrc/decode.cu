@@ -1053,11 +1053,11 @@ static int launch_decode(DecodeArgs &a, int item_ctas, const CUtensorMap &map, c
     const int n_items = a.n_seqs * a.Hkv * a.blocks;
     const size_t per_warp = warp_smem<DB>(a.q_bytes), smem = 1024 + per_warp * (item_ctas ? kItemWarps : 1);
     if (item_ctas) {
-        LLMS_CUDA_TRY(cudaFuncSetAttribute(decode_kernel<BF, DB, MODE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        LLMS_CUDA_TRY((allow_shared_memory<decode_kernel<BF, DB, MODE, true>>()));
         LLMS_CUDA_TRY(launch_dependent_cluster(decode_kernel<BF, DB, MODE, true>, dim3(n_items * item_ctas), dim3(kItemWarps * 32), smem, item_ctas, st,
                                                a, map));
     } else {
-        LLMS_CUDA_TRY(cudaFuncSetAttribute(decode_kernel<BF, DB, MODE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        LLMS_CUDA_TRY((allow_shared_memory<decode_kernel<BF, DB, MODE, false>>()));
         LLMS_CUDA_TRY(launch_dependent(decode_kernel<BF, DB, MODE, false>, dim3(a.grid_runs), dim3(32), smem, st, a, map));
     }
     return LLMS_OK;

@@ -549,7 +549,9 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     while ((1 << a.select_shift) < parts) ++a.select_shift;
     while ((32 << a.warps_shift) < threads) ++a.warps_shift;
     void (*select)(EvictArgs) = shared ? select_kernel<true, false> : (fused ? select_kernel<false, true> : select_kernel<false, false>);
-    LLMS_CUDA_TRY(cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    cudaError_t (*allow)() = shared ? allow_shared_memory<select_kernel<true, false>>
+                                    : (fused ? allow_shared_memory<select_kernel<false, true>> : allow_shared_memory<select_kernel<false, false>>);
+    LLMS_CUDA_TRY(allow());
     LLMS_CUDA_TRY(launch_dependent_cluster(select, dim3(a.Hkv * parts, n_seqs, a.L), dim3(threads), smem, parts, st, a));
     if (fused) return LLMS_OK;
 

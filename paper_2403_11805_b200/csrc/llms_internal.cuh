@@ -5,6 +5,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "llms.h"
 
 namespace llms {
@@ -39,6 +41,26 @@ inline cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 bl
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
+// Lets `Kernel` be launched with all the dynamic shared memory that a block of the current device can have.  The limit belongs to
+// the kernel, not to a launch: it is raised once per device and never lowered.  Set by every call to the call's own need,
+// it could be lowered by a call of another host thread between this one's setting and its launch, which is then refused.
+template <auto Kernel>
+inline cudaError_t allow_shared_memory()
+{
+    static std::atomic<uint64_t> raised{0};           // a bit per device
+    int device = 0, most = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (raised.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    cudaFuncAttributes attr;
+    if ((e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, device)) != cudaSuccess) return e;
+    if ((e = cudaFuncGetAttributes(&attr, Kernel)) != cudaSuccess) return e;
+    e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)attr.sharedSizeBytes);
+    if (e == cudaSuccess) raised.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
 #ifdef __CUDACC__
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

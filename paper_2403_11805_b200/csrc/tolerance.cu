@@ -787,7 +787,7 @@ static int launch_logits_tc_inst(const TolArgs &a, const CUtensorMap &map_k, con
     const size_t operand = (size_t)(D / 64) * kTcBlockBytes, stage = (size_t)(D / 64) * kTcWideBlockBytes;
     const int n_stages = (int)std::min<size_t>(8, (227 * 1024 - 2 * operand - sizeof(TcBarriers) - 1024) / stage);
     const size_t smem = 1024 + 2 * operand + (size_t)n_stages * stage + sizeof(TcBarriers);
-    LLMS_CUDA_TRY(cudaFuncSetAttribute(logits_tc_kernel<SEG, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    LLMS_CUDA_TRY((allow_shared_memory<logits_tc_kernel<SEG, D, R>>()));
     logits_tc_kernel<SEG, D, R><<<a.tc_grid, kTcThreads, smem, st>>>(a, map_k, map_q, n_stages);
     return LLMS_OK;
 }
@@ -949,8 +949,8 @@ int llms::chunk_tolerance_impl(const llms_kv_desc *desc, const void *kv, const v
         const dim3 grid(splits, pairs);
 #define LLMS_LAUNCH_MMA_G(S, DD, G)                                                                                                  \
     do {                                                                                                                             \
-        LLMS_CUDA_TRY(cudaFuncSetAttribute(logits_mma_kernel<S, DD, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)mma_smem)); \
-        logits_mma_kernel<S, DD, G><<<grid, cta_warps * 32, mma_smem, st>>>(a);                                                     \
+        LLMS_CUDA_TRY((allow_shared_memory<logits_mma_kernel<S, DD, G>>()));                                                         \
+        logits_mma_kernel<S, DD, G><<<grid, cta_warps * 32, mma_smem, st>>>(a);                                                      \
     } while (0)
 #define LLMS_LAUNCH_MMA(S, DD)                        \
     do {                                              \
@@ -981,7 +981,7 @@ int llms::chunk_tolerance_impl(const llms_kv_desc *desc, const void *kv, const v
         const dim3 grid((a.T + kTokThreads - 1) / kTokThreads, a.L * a.Hkv);
 #define LLMS_LAUNCH_LOGITS(S)                                                                                   \
     case S:                                                                                                     \
-        LLMS_CUDA_TRY(cudaFuncSetAttribute(logits_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)q_bytes)); \
+        LLMS_CUDA_TRY(allow_shared_memory<logits_kernel<S>>());                                                 \
         logits_kernel<S><<<grid, kTokThreads, q_bytes, st>>>(a);                                                \
         break;
         switch (t.SEG) {
