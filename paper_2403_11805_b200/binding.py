@@ -387,6 +387,11 @@ def _current(stream):
     return device, stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def current_stream():
+    """Address of the current stream."""
+    return _current(None)[1]
+
+
 def _is_whole(x, shape, dtype, device):
     return x.shape == shape and x.dtype is dtype and x.get_device() == device and x.is_contiguous()
 

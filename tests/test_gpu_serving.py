@@ -190,3 +190,111 @@ def test_more_reclaims_in_a_step_than_the_pool_has_workspaces():
         for i, r in enumerate(app.rows(c)):
             if r in records:
                 assert np.array_equal(bits_view(app.context_kv(c))[..., i * 16:(i + 1) * 16, :], records[r])
+
+
+def reference_step(bt, sh, qkv, layer):
+    """The reference batch with a token's rows, and what the layer's decode call has to give."""
+    bt.qkv = qkv
+    bt.q, bt.k_new, bt.v_new = qkv.split([sh.n_q_heads, sh.n_kv_heads, sh.n_kv_heads], dim=1)
+    return attend(bt, layer, append=True, mass_in=bt.mass[layer], mass_before=bt.mass[layer])
+
+
+def pool_of_modified_chunks(n_slots=40):
+    """Contexts of 16 chunks, n_slots of them full of modified ones, context 2 down to a chunk."""
+    sh = synth.KVShape("apps", 1, 2, 8, 64, 256, 16, 64, window=4, seed=6, n_contexts=5)
+    app = MultiApp(sh, n_slots=n_slots, seed=2)
+    app.build()
+    chosen = []
+    app.draw_contexts = lambda k: list(chosen)
+
+    def step(c, serve=None):
+        chosen[:] = [c]
+        app.step(k=1, serve=serve)
+        consistent(app)
+
+    for c in (2, 3, 4):
+        step(c, (lambda s: s.shrink(16, 1)) if c == 2 else None)
+    app.clean[:] = False
+    return sh, app, step
+
+
+def test_serving_on_a_stream_of_its_own():
+    """The callback's stream is late by a delay in front of every token, and every growth reclaims a chunk of others: what leaves
+    is what lay in the slots, and attention sees the rows that were stored."""
+    sh, app, step = pool_of_modified_chunks()
+    side = torch.cuda.Stream()
+    g = torch.Generator().manual_seed(3)
+    left = {}
+
+    def serve(s):
+        with torch.cuda.stream(side):
+            for _ in range(7 * 16):
+                grows = s.lengths[0] % 16 == 0
+                if grows:
+                    side.synchronize()
+                    torch.cuda.synchronize()
+                    before, slots = app.pool.cpu(), {int(r): int(app.slot[r]) for r in np.flatnonzero(app.slot >= 0)}
+                torch.cuda._sleep(200000)
+                s.advance()
+                if grows:
+                    for r, slot in slots.items():
+                        if app.slot[r] < 0:
+                            left[r] = before[..., slot * 16:(slot + 1) * 16, :]
+                torch.cuda._sleep(200000)
+                qkv = torch.randn(1, 12, 64, generator=g).half()
+                dev = qkv.cuda(non_blocking=True).split([8, 2, 2], dim=1)
+                if grows:                                     # with a reference: everything in between has been waited for then
+                    side.synchronize()
+                    bt = batch_of(s, sh, app)
+                    want, _, wmass, wkv, (ot, _, mt) = reference_step(bt, sh, qkv, 0)
+                out = s.decode(0, *dev)
+                if grows:
+                    assert ((out.cpu().double() - want).abs() <= ot).all()
+                    assert ((s.mass[0].cpu().double() - wmass).abs() <= mt).all()
+                    assert torch.equal(bits(app.pool.cpu()), bits(wkv))
+
+    step(2, serve)
+    app.finish()
+    assert len(left) >= 4
+    one = odesc(sh.with_(n_tokens=16))
+    arena = app.arena.numpy()
+    for r, chunk in left.items():
+        buf, meta = oracle.compress_chunks(one, np.ascontiguousarray(bits_view(chunk)), [0], [int(app.table["bits"][r])])
+        off = int(app.arena_off[r])
+        assert app.checksum[r] == meta[0]["checksum"] and np.array_equal(arena[off:off + buf.size], buf), r
+    for c in (3, 4):
+        step(c)
+
+
+def test_a_captured_decode_replayed_between_growth_and_shrinking():
+    sh, app, step = pool_of_modified_chunks()
+    g = torch.Generator().manual_seed(4)
+
+    def serve(s):
+        qkv = torch.zeros(1, 12, 64, dtype=torch.float16, device="cuda")
+        q, k, v = qkv.split([8, 2, 2], dim=1)
+        out = torch.zeros(1, 8, 64, dtype=torch.float16, device="cuda")
+        s.advance()
+        s.decode(0, q, k, v, out)
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            s.decode(0, q, k, v, out)
+        with torch.cuda.stream(side):
+            for i in range(60):
+                s.advance()
+                if i == 40:
+                    s.shrink(24, 4)
+                    s.advance()
+                token = torch.randn(1, 12, 64, generator=g).half()
+                qkv.copy_(token)
+                side.synchronize()
+                bt = batch_of(s, sh, app)
+                want, _, wmass, wkv, (ot, _, mt) = reference_step(bt, sh, token, 0)
+                graph.replay()
+                assert ((out.cpu().double() - want).abs() <= ot).all()
+                assert ((s.mass[0].cpu().double() - wmass).abs() <= mt).all()
+                assert torch.equal(bits(app.pool.cpu()), bits(wkv))
+
+    step(2, serve)
+    assert app.lengths[2] == 24 + 20

@@ -3,6 +3,7 @@
 Work that the module queues runs when the host waits for it and not before, in the order in which it was queued, as on a device
 that is always behind: meta arrays and workspaces hold results only then.  A chunk's content is one number, which is its record
 and its checksum too."""
+import contextlib
 import types
 
 import numpy as np
@@ -18,6 +19,14 @@ class Device:
     def __init__(self):
         self.queue, self.slots, self.staged, self.arena, self.corrupt, self.fresh = [], {}, {}, {}, {}, 1000
         self.waits = 0
+        self.main = Stream(0, self)
+        self.current, self.log = self.main, []               # the current stream; (what, on which stream) in the order of the calls
+
+    @contextlib.contextmanager
+    def stream(self, s):
+        self.current, before = s, self.current
+        yield
+        self.current = before
 
     def wait(self, *_):
         self.waits += 1
@@ -32,6 +41,7 @@ class Device:
     # ---- the binding's calls
     def compress_chunks(self, desc, kv, ids, bits, out, meta, ws, **_):
         ids = [int(i) for i in ids]
+        self.log.append(("compress", self.current.cuda_stream))
 
         def work():
             for i, slot in enumerate(ids):
@@ -77,12 +87,14 @@ class Event:
 
 
 class Stream:
-    cuda_stream = 0
+    def __init__(self, address=0, device=None):
+        self.cuda_stream, self.device = address, device
 
     def wait_event(self, *_):
         pass
 
-    wait_stream = wait_event
+    def wait_stream(self, other):
+        self.device.log.append(("wait", self.cuda_stream, other.cuda_stream))
 
 
 @pytest.fixture
@@ -94,8 +106,8 @@ def device(monkeypatch):
             return getattr(torch, name)(*shape, **kw)
         return make
 
-    stream = Stream()
-    cuda = types.SimpleNamespace(synchronize=dev.wait, current_stream=lambda *_: stream, Stream=Stream, Event=lambda **_: Event(dev))
+    cuda = types.SimpleNamespace(synchronize=dev.wait, current_stream=lambda *_: dev.current, stream=dev.stream, Stream=Stream,
+                                 Event=lambda **_: Event(dev))
     fake = types.SimpleNamespace(cuda=cuda, **{n: made(n) for n in ("zeros", "empty", "full")},
                                  **{n: getattr(torch, n) for n in ("from_numpy", "empty_like", "cat", "uint8", "int32", "float16", "float32")})
     monkeypatch.setattr(multiapp, "torch", fake)
@@ -105,6 +117,7 @@ def device(monkeypatch):
     for name in ("compress_chunks", "swap_out", "swap_in", "decompress_chunks", "codec_corrupt_count", "evict_tokens"):
         monkeypatch.setattr(B, name, getattr(dev, name))
     monkeypatch.setattr(B, "new_event", lambda *_: Event(dev))
+    monkeypatch.setattr(B, "current_stream", lambda: dev.current.cuda_stream)
     return dev
 
 
@@ -197,3 +210,27 @@ def test_a_step_of_few_reclaims_waits_at_its_end_only(device):
     waits, inside = device.waits, []
     step(app, [2], lambda s: (grow(device, app, 40)(s), inside.append(device.waits - waits)))
     assert inside == [0]
+
+
+def test_a_callback_on_a_stream_of_its_own(device):
+    """What growth and shrinking queue goes to the pool's stream, behind the caller's work and before its next."""
+    app, _ = crowded(device)
+    side = Stream(7, device)
+
+    def serve(s):
+        device.log.clear()
+        with device.stream(side):
+            grow(device, app, 3)(s)
+            grown = list(device.log)
+            device.log.clear()
+            s.shrink(16, 1)
+        assert [e for e in grown if e[0] == "compress"] == [("compress", 0)] * 3
+        for i, e in enumerate(grown):
+            if e[0] == "compress":
+                assert grown[i - 1] == ("wait", 0, 7) and grown[i + 1] == ("wait", 7, 0)
+        assert device.log == [("wait", 0, 7), ("wait", 7, 0)]
+
+    step(app, [2], serve)
+    device.log.clear()
+    step(app, [1], lambda s: s.shrink(1600, 1))              # on the pool's own stream nothing has to be ordered
+    assert not [e for e in device.log if e[0] == "wait"]
