@@ -24,6 +24,7 @@ class Serving:
         sh = app.shape
         n, self.capacity = len(self.ctxs), app.cpc * sh.chunk_len
         self._main = app.main.cuda_stream
+        self.closed = False
         self.lengths = np.array([app.lengths[c] for c in self.ctxs], dtype=np.int64)
         self.host_table = np.full((n, app.cpc), -1, dtype=np.int32)
         for i, c in enumerate(self.ctxs):
@@ -50,8 +51,13 @@ class Serving:
     def _on_pool_stream(self):
         return contextlib.nullcontext() if B.current_stream() == self._main else self._on_another_stream()
 
+    def _check_open(self):
+        if self.closed:
+            raise RuntimeError("the step that this batch was served in has ended: its chunks may be others' by now")
+
     def advance(self):
         """Room for one more token per context: its length grows by one, by a new chunk where the last one is full."""
+        self._check_open()
         app = self.app
         if (self.lengths >= self.capacity).any():
             raise RuntimeError("a context is full: shrink it before it takes more tokens")
@@ -71,6 +77,7 @@ class Serving:
         """Attention of the newest token of every context in one layer: q [n, n_q_heads, head_dim], k_new and v_new
         [n, n_kv_heads, head_dim], fp16 (views of one projection's output will do).  Stores k_new and v_new as the newest
         token's rows, adds the attention weights to self.mass, returns the output rows."""
+        self._check_open()
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
         if B.current_stream() != self._main and not torch.cuda.is_current_stream_capturing():
             with self._on_another_stream():
@@ -86,6 +93,7 @@ class Serving:
     def shrink(self, budget, recent):
         """Every context longer than `budget` keeps, per layer and KV head, that many tokens: the last `recent` ones and those
         with the largest accumulated weight.  Returns the kept positions [n_layers, n, n_kv_heads, budget] (device)."""
+        self._check_open()
         app = self.app
         sh = app.shape
         kept = torch.empty(sh.n_layers, len(self.ctxs), sh.n_kv_heads, budget, dtype=torch.int32, device="cuda")
@@ -102,6 +110,8 @@ class Serving:
         return kept
 
     def close(self):
-        """The contexts' lengths are what the pool's bookkeeping goes by from now on."""
+        """The end of the step: the contexts' lengths are what the pool's bookkeeping goes by from now on, and the batch is no
+        longer to be used (nor graphs captured from it)."""
+        self.closed = True
         for i, c in enumerate(self.ctxs):
             self.app.lengths[c] = int(self.lengths[i])

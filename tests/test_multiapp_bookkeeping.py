@@ -234,3 +234,15 @@ def test_a_callback_on_a_stream_of_its_own(device):
     device.log.clear()
     step(app, [1], lambda s: s.shrink(1600, 1))              # on the pool's own stream nothing has to be ordered
     assert not [e for e in device.log if e[0] == "wait"]
+
+
+def test_a_batch_is_not_used_behind_its_step(device):
+    app, _ = crowded(device)
+    kept = []
+    step(app, [2], kept.append)
+    lengths, slots = list(app.lengths), app.slot.copy()
+    s = kept[0]
+    for use in (s.advance, lambda: s.decode(0, None, None, None), lambda: s.shrink(1, 1)):
+        with pytest.raises(RuntimeError, match="has ended"):
+            use()
+    assert app.lengths == lengths and np.array_equal(app.slot, slots)
