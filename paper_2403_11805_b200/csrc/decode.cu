@@ -190,13 +190,17 @@ __device__ __forceinline__ float2 unpack(uint32_t x)
     return __half22float2(h);
 }
 
+// A channel of the output: its weighted sum times the inverse of the weights' sum.  A row of no weight at all is 0 even where a value is
+// infinite or NaN, whose product with a weight of 0 has made the sum NaN.
+__device__ __forceinline__ float channel(float acc, float inv) { return inv == 0.0f ? 0.0f : acc * inv; }
+
 // Four channels of a finished row (16-bit values), and with the first ones the row's log-sum.
 template <bool BF>
 __device__ __forceinline__ void finish_row(const DecodeArgs &a, int64_t row, int c, const float (&acc)[4], float top, float sum)
 {
     const float inv = sum == 0.0f ? 0.0f : (1.0f / kLift) / sum;
     if (c < a.d) {
-        const uint2 x = make_uint2(pack_round<BF>(acc[0] * inv, acc[1] * inv), pack_round<BF>(acc[2] * inv, acc[3] * inv));
+        const uint2 x = make_uint2(pack_round<BF>(channel(acc[0], inv), channel(acc[1], inv)), pack_round<BF>(channel(acc[2], inv), channel(acc[3], inv)));
         *reinterpret_cast<uint2 *>(a.out + row * a.d + c) = x;
     }
     if (c == 0) {
@@ -784,7 +788,7 @@ __global__ void __launch_bounds__(ITEM ? kItemWarps * 32 : 32) decode_kernel(con
                     for (int t = 0; t < KS; ++t)
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const uint32_t x = transpose8x8(pack_round<BF>(o[t][nt][2 * i] * inv[0], o[t][nt][2 * i + 1] * inv[1]));
+                            const uint32_t x = transpose8x8(pack_round<BF>(channel(o[t][nt][2 * i], inv[0]), channel(o[t][nt][2 * i + 1], inv[1])));
                             if (r < have && t * 16 + i * 8 + (lane & 3) * 2 < a.d) *reinterpret_cast<uint32_t *>(to + t * 16 + i * 8) = x;
                         }
 #pragma unroll

@@ -177,6 +177,22 @@ def test_rows_whose_logits_are_all_minus_infinity_are_empty():
         assert torch.equal(mass[at + b, :, :bt.lens[at + b]], bt.mass[0][at + b, :, :bt.lens[at + b]])
 
 
+@pytest.mark.parametrize("form", ["cluster", "whole_in_a_run", "over_runs", "cluster_of_parts"])
+def test_rows_of_no_weight_are_zero_whatever_their_values(form):
+    """All logits -inf: the row is 0 also where values are infinite or NaN."""
+    length = {"cluster": 20, "whole_in_a_run": 20, "over_runs": 300, "cluster_of_parts": 100}[form]
+    bt = Batch([length, length], heads=1, seed=1, group=3)
+    bt.q[:] = 1.0
+    bt.kv[0, 0, 0, bt.rows(0)] = -math.inf
+    bt.kv[0, 1, 0, bt.rows(0)] = math.inf
+    bt.kv[0, 1, 0, bt.rows(0)[5]] = math.nan
+    at = 0 if form.startswith("cluster") else padded(bt)
+    out, lse, mass, _ = call(bt, mass="add")
+    assert (lse[at] == -math.inf).all() and torch.equal(mass[at, :, :length], bt.mass[0][at, :, :length])
+    assert (out[at] == 0).all()
+    assert out[at + 1].isfinite().all() and lse[at + 1].isfinite().all()
+
+
 @pytest.mark.parametrize("bad_len", [1000, -3])
 def test_invalid_lengths_and_slots_answer_nan_and_touch_nothing(bad_len):
     bt = Batch([30, 40, 50, 60, 20], seed=12, group=2)
