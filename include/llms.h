@@ -295,7 +295,8 @@ typedef enum llms_dtype { LLMS_F16 = 0, LLMS_BF16 = 1 } llms_dtype;
  * and, where mass_out is given, for every t < lens[b] (weight 0 outside the window)
  *     mass_out[b][h][t] = mass_in[b][h][t] + sum over those query heads of exp(s_t - lse).
  * A sequence without tokens, or with nothing but weights of 0 (all s_t = -inf), gives out = 0 and lse = -inf.  Sums are kept
- * in binary32 (the products of the weights with V take the weights as a pair of 16-bit values, 16 or more bits together).
+ * in binary32.  The products with V take a weight as a pair of 16-bit values: off by less than 2^-20 of the weight with
+ * LLMS_F16, 2^-15.6 with LLMS_BF16; with LLMS_F16 also by up to 2^-31 of the row's largest weight, which smaller ones lose.
  *   dtype     type of kv, q, k_new, v_new and out (llms_dtype; the codec calls take LLMS_F16 only)
  *   kv        device, the pool, 16-byte aligned
  *   q         device [n_seqs] rows of n_q_heads * head_dim elements, q_stride elements apart; 16-byte aligned, q_stride a
