@@ -129,6 +129,18 @@ def test_masses_up_to_and_beyond_a_cluster_s_shared_memory(tokens):
     check(bt, bt.mass, tokens // 3, 10, mass_out="same")
 
 
+@pytest.mark.parametrize("where", ["in_place", "other_slots"])
+@pytest.mark.parametrize("lens", [[16500, 20000, 16384, 16385], [17001]], ids=["several_long", "one_long"])
+def test_one_kernel_whose_masses_do_not_fit_shared_memory(lens, where):
+    """More items than the GPU takes at once, and a length bound beyond what a CTA holds: masses are read again in every pass, and
+    written over in place tile by tile."""
+    bt = Batch(lens + [(i * 31) % 90 for i in range(100)], heads=7, dim=16, seed=len(lens))
+    dst = other_slots(bt, 9000) if where == "other_slots" else None
+    check(bt, bt.mass, 9000, 70, dst, mass_out="same")
+    check(bt, (bt.mass * 0.3).round(), 9000, 70, dst, mass_out="same")
+    check(bt, bt.mass, 9000, 70, dst)
+
+
 VALUES = {
     "all_equal": lambda m: torch.full_like(m, 2.5), "all_zero": lambda m: torch.zeros_like(m),
     "few_values": lambda m: (m * 0.2).round(), "signed_zeros": lambda m: torch.where(m > 1, 0.0, -0.0),
