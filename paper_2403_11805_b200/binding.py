@@ -446,6 +446,8 @@ def decode_attention(desc, layer, kv, q, chunk_table, lens, max_len, out, worksp
         q_stride, table_stride = hq * d, chunks
     if chunks * desc.chunk_len < max_len:
         _refuse(what, device, f"max_len {max_len} is more than a table row's chunks of {desc.chunk_len} hold", chunk_table=chunk_table)
+    if (layer | window) >> 31:                                # negative, or not an int of the C call
+        _refuse(what, device, f"layer {layer}, window {window}")
     k_ptr = v_ptr = in_ptr = out_ptr = None
     new_stride = mass_stride = 0
     if k_new is not None or v_new is not None:
@@ -491,6 +493,8 @@ def evict_tokens(desc, kv, mass, chunk_table, lens, max_len, budget, recent, kep
     chunks, dst_ptr, dst_stride = chunk_table.shape[1], None, 0
     if chunks * desc.chunk_len < max_len:
         _refuse(what, device, f"max_len {max_len} is more than a table row's chunks of {desc.chunk_len} hold", chunk_table=chunk_table)
+    if (budget | recent) >> 31:                               # negative, or not an int of the C call
+        _refuse(what, device, f"budget {budget}, recent {recent}")
     if dst_table is not None:
         if not (_is_batch(dst_table, lens, device) and dst_table.shape[1] * desc.chunk_len >= min(budget, max_len)):
             _refuse(what, device, f"dst_table int32 [{n}, chunks] with room for {min(budget, max_len)} tokens", dst_table=dst_table)

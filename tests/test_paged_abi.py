@@ -88,6 +88,46 @@ def test_a_table_as_its_own_destination_keeps_its_stride():
     assert evict(dst_table=A, table_stride=5, dst_stride=8) == INVALID
 
 
+@pytest.fixture
+def on_the_host(monkeypatch):
+    """The binding's checks over tensors in host memory; the C calls are only noted."""
+    import torch
+    called = []
+    fake = type("Lib", (), {name: staticmethod(lambda *a, name=name: called.append(name) or 0) for name in ("llms_decode_attention", "llms_evict_tokens")})
+    fake.llms_strerror = B.lib().llms_strerror
+    B._CACHE_TYPES.update({torch.float16: B.DTYPE_F16, torch.bfloat16: B.DTYPE_BF16})
+    monkeypatch.setattr(B, "_torch", torch)
+    monkeypatch.setattr(B, "_current", lambda stream: (-1, 0))               # where host tensors say they are
+    monkeypatch.setattr(B, "_lib", fake)
+    return called
+
+
+def binding_calls():
+    import torch
+    kv, i32 = torch.zeros(2, 2, 4, 160, 64, dtype=torch.float16), dict(dtype=torch.int32)
+    table, lens = torch.zeros(3, 5, **i32), torch.zeros(3, **i32)
+    q, out, mass = torch.zeros(3, 8, 64, dtype=torch.float16), torch.zeros(3, 8, 64, dtype=torch.float16), torch.zeros(2, 3, 4, 80)
+    return (lambda **kw: B.decode_attention(pool(), **{**dict(layer=0, kv=kv, q=q, chunk_table=table, lens=lens, max_len=80, out=out,
+                                                              workspace=torch.zeros(1 << 20, dtype=torch.uint8)), **kw}),
+            lambda **kw: B.evict_tokens(pool(), **{**dict(kv=kv, mass=mass, chunk_table=table, lens=lens, max_len=80, budget=20, recent=4,
+                                                          kept=torch.zeros(2, 3, 4, 20, **i32), new_lens=torch.zeros(3, **i32)), **kw}))
+
+
+@pytest.mark.parametrize("which,kw", [
+    (0, dict(window=1 << 32)), (0, dict(window=(1 << 32) + 16)), (0, dict(window=1 << 31)), (0, dict(layer=1 << 32)), (0, dict(layer=-(1 << 32))),
+    (1, dict(recent=1 << 32)), (1, dict(recent=-(1 << 32) + 2)),
+], ids=str)
+def test_numbers_beyond_the_c_call_s_are_refused(which, kw, on_the_host):
+    """They would reach the call cut off to 32 bits, as other numbers."""
+    calls = binding_calls()
+    for call in calls:
+        call()
+    assert on_the_host == ["llms_decode_attention", "llms_evict_tokens"]
+    with pytest.raises(B.LlmsError) as e:
+        calls[which](**kw)
+    assert e.value.status == INVALID and len(on_the_host) == 2
+
+
 def test_an_empty_batch_does_nothing():
     assert decode(n_seqs=0, q=None, out=None) == B.OK
     assert evict(n_seqs=0, kept=None) == B.OK
