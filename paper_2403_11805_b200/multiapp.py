@@ -37,7 +37,8 @@ class MultiApp:
         self.table["ctx_id"] = np.repeat(np.arange(self.n_ctx), self.cpc)
         self.table["chunk_id"] = np.tile(np.arange(self.cpc), self.n_ctx)
         self.slot = np.full(n, -1, dtype=np.int64)
-        self.lengths = [shape.n_tokens] * self.n_ctx   # tokens per context; chunks behind them hold nothing (Serving.shrink)
+        # tokens per context: whole chunks; chunks behind them hold nothing (Serving.shrink)
+        self.lengths = [self.cpc * shape.chunk_len] * self.n_ctx
         self.free = list(range(n_slots - 1, -1, -1))
         self.checksum = np.zeros(n, dtype=np.uint32)
         self.clean = np.zeros(n, dtype=bool)      # the record in the arena matches what sits in the slot

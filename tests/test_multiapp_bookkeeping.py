@@ -246,3 +246,22 @@ def test_a_batch_is_not_used_behind_its_step(device):
         with pytest.raises(RuntimeError, match="has ended"):
             use()
     assert app.lengths == lengths and np.array_equal(app.slot, slots)
+
+
+def test_contexts_whose_last_chunk_is_not_whole(device):
+    """The pool holds whole chunks; the tokens behind the last one take no part, and no rows of the next context."""
+    sh = synth.KVShape("apps", 1, 1, 1, 16, 5 * 16 + 7, 16, 16, window=4, seed=1, n_contexts=4)
+    app = multiapp.MultiApp(sh, n_slots=10, seed=1)
+    app._alloc_buffers()
+    for c in range(4):
+        bits, _ = B.assign_bits(np.arange(5, dtype=np.float32), app.frac)
+        app._place_in_arena(c, bits)
+    for row in range(20):
+        app.checksum[row] = device.arena[int(app.arena_off[row])] = device.new_content()
+    for c in (2, 3, 0, 1):
+        assert app.rows(c).tolist() == list(range(5 * c, 5 * c + 5))
+        lengths = []
+        app.draw_contexts = lambda k, c=c: [c]
+        app.step(k=1, serve=lambda s: lengths.extend(s.lengths))
+        assert lengths == [80] and app.table["resident"][5 * c:5 * c + 5].all() and app.table["resident"].sum() <= 10
+        assert set(np.flatnonzero(app.table["last_access_step"] == app.step_no)) == set(range(5 * c, 5 * c + 5))
