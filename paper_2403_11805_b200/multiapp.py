@@ -258,6 +258,9 @@ class MultiApp:
         """Rows of the chunk table that hold tokens of context c."""
         return np.arange(c * self.cpc, c * self.cpc + -(-self.lengths[c] // self.shape.chunk_len))
 
+    def _rows_of(self, ctxs):
+        return np.concatenate([np.arange(0)] + [self.rows(c) for c in ctxs])
+
     def take_slots(self, n):
         """n free slots; chunks of unlocked contexts are reclaimed in LCTRU order if there are not enough."""
         need = n - len(self.free)
@@ -298,13 +301,14 @@ class MultiApp:
 
     def step(self, k=8, serve=None):
         """Serve k contexts: lock, evict in LCTRU order as far as needed, load, touch, unlock.  serve: called with a Serving
-        of the contexts while their working sets are resident and locked."""
+        of the contexts while their working sets are resident and locked (not called when every context is resident already
+        and none is drawn).  Returns the contexts."""
         self.step_no += 1
         if not hasattr(self, "_ev_t0"):
             self._ev_t0, self._ev_ready = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         self._ev_t0.record(self.main)
         ctxs = self.draw_contexts(k)
-        locked_rows = np.concatenate([self.rows(c) for c in ctxs])
+        locked_rows = self._rows_of(ctxs)
         self.table["locked"][locked_rows] = 1            # working-set lock
         for c in ctxs:
             rows = self.rows(c)
@@ -322,13 +326,13 @@ class MultiApp:
             self.table["last_access_step"][rows] = self.step_no
         self._ev_ready.record(self.main)                 # the working sets are resident: inference could start
         try:
-            if serve is not None:
+            if serve is not None and ctxs:
                 batch = Serving(self, ctxs)
                 try:
                     serve(batch)
                 finally:
                     batch.close()                        # what it did to the contexts stands, also if it raised
-                    locked_rows = np.concatenate([self.rows(c) for c in ctxs])
+                    locked_rows = self._rows_of(ctxs)
         finally:
             self._leave(locked_rows)
         self.ready_ms.append(self._ev_t0.elapsed_time(self._ev_ready))

@@ -265,3 +265,28 @@ def test_contexts_whose_last_chunk_is_not_whole(device):
         app.step(k=1, serve=lambda s: lengths.extend(s.lengths))
         assert lengths == [80] and app.table["resident"][5 * c:5 * c + 5].all() and app.table["resident"].sum() <= 10
         assert set(np.flatnonzero(app.table["last_access_step"] == app.step_no)) == set(range(5 * c, 5 * c + 5))
+
+
+def test_a_step_with_every_context_resident_serves_none(device):
+    """Shrunk contexts all fit: nothing is drawn, and that is an empty step, not an error."""
+    app = pool(device)
+    for c in range(4):
+        step(app, [c], lambda s: s.shrink(20, 1))
+    del app.draw_contexts
+    for c in (0, 1):                                          # whatever is out comes in
+        app.step(k=4)
+    assert all(app.table["resident"][app.rows(c)].all() for c in range(4))
+    served, before = [], (app.slot.copy(), list(app.free), app.table.copy())
+    assert app.step(k=2, serve=served.append) == [] and not served
+    assert np.array_equal(app.slot, before[0]) and app.free == before[1] and np.array_equal(app.table, before[2])
+
+
+def test_an_empty_step_settles_what_the_last_one_left(device):
+    app = pool(device, aot=True)
+    for c in range(4):
+        step(app, [c], lambda s: s.shrink(20, 1))
+    del app.draw_contexts
+    app.step(k=4)
+    app.step(k=4)
+    assert device.queue == [] and not app._pending
+    assert all(app.checksum[r] == device.slots[int(app.slot[r])] for c in range(4) for r in app.rows(c) if app.slot[r] >= 0)
