@@ -436,11 +436,11 @@ def decode_attention(desc, layer, kv, q, chunk_table, lens, max_len, out, worksp
     chunks = chunk_table.shape[-1]
     if not (lens.dtype is i32 and lens.get_device() == device and lens.is_contiguous() and lens.dim() == 1
             and chunk_table.dtype is i32 and chunk_table.get_device() == device and (table_entry == 1 or chunks == 1)
-            and chunk_table.shape[0] == n and kv.get_device() == device and workspace.get_device() == device
+            and chunk_table.shape[0] == n and kv.get_device() == device and workspace.get_device() == device and workspace.is_contiguous()
             and q.dtype is dtype and q.get_device() == device and q.shape == (n, hq, d) and q_channel == 1 and (q_head == d or hq == 1)
             and out.dtype is dtype and out.get_device() == device and out.shape == (n, hq, d) and out.is_contiguous()
             and (lse is None or _is_whole(lse, (n, hq), f32, device))):
-        _refuse(what, device, f"kv on this device, chunk_table int32 [{n}, chunks], lens int32 [{n}], q and out [{n}, {hq}, {d}] of kv's type, "
+        _refuse(what, device, f"kv and a contiguous workspace on this device, chunk_table int32 [{n}, chunks], lens int32 [{n}], q and out [{n}, {hq}, {d}] of kv's type, "
                 f"lse float32 [{n}, {hq}]", kv=kv, chunk_table=chunk_table, lens=lens, q=q, out=out, lse=lse, workspace=workspace)
     if n <= 1:
         q_stride, table_stride = hq * d, chunks

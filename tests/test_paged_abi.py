@@ -128,6 +128,19 @@ def test_numbers_beyond_the_c_call_s_are_refused(which, kw, on_the_host):
     assert e.value.status == INVALID and len(on_the_host) == 2
 
 
+def test_a_workspace_without_the_bytes_that_its_size_says_is_refused(on_the_host):
+    """A view's nbytes counts its elements, wherever they lie."""
+    import torch
+    decode_call, _ = binding_calls()
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 21, dtype=torch.uint8)[::2]):
+        with pytest.raises(B.LlmsError) as e:
+            decode_call(workspace=ws)
+        assert e.value.status == INVALID
+    assert on_the_host == []
+    decode_call(workspace=torch.zeros(256, 4096, dtype=torch.uint8))
+    assert on_the_host == ["llms_decode_attention"]
+
+
 def test_an_empty_batch_does_nothing():
     assert decode(n_seqs=0, q=None, out=None) == B.OK
     assert evict(n_seqs=0, kept=None) == B.OK
