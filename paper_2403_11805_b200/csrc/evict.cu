@@ -555,7 +555,7 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
     LLMS_CUDA_TRY(launch_dependent_cluster(select, dim3(a.Hkv * parts, n_seqs, a.L), dim3(threads), smem, parts, st, a));
     if (fused) return LLMS_OK;
 
-    constexpr int kFillCtas = 296;                // in place, a slab is shared by a cluster until there are so many CTAs (see move_kernel)
+    const int fill_ctas = 2 * sm_count();         // in place, a slab is shared by a cluster until there are so many CTAs (see move_kernel)
     const int batch = kMoveThreads / (a.d / 8) * in_flight(false), most_batches = (most + batch - 1) / batch;
     void (*kernel)(EvictArgs);
     if (dst_table) {
@@ -564,7 +564,7 @@ extern "C" int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float
         kernel = move_kernel<false, false>;
     } else {
         a.parts = 1;
-        while (a.parts < kMaxCluster && items * 2 * a.parts < kFillCtas && a.parts < most_batches) a.parts *= 2;
+        while (a.parts < kMaxCluster && items * 2 * a.parts < fill_ctas && a.parts < most_batches) a.parts *= 2;
         kernel = a.parts > 1 ? move_kernel<true, true> : move_kernel<true, false>;
     }
     if ((int64_t)a.Hkv * 2 * a.parts > 0x7fffffff) return LLMS_ERR_UNSUPPORTED;
