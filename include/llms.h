@@ -278,7 +278,7 @@ int llms_compress_context(const llms_kv_desc *desc, const void *kv, const void *
 /* What a served context does between Load and Reclaim (Sec. 3.1: inference runs on the resident chunks): a new token
  * attends to the context's cached tokens, and a context may be shrunk to the tokens that attention weighs most.  Both
  * calls work on a pool of chunk slots (`desc` as for the codec calls, n_tokens = slots * chunk_len; group_size and
- * quant_mode are not used) and on a batch of sequences, each with a row of a chunk table:
+ * quant_mode are checked but have no influence) and on a batch of sequences, each with a row of a chunk table:
  *   chunk_table  device int32 [n_seqs][table_stride]: slot of chunk i of sequence b.  Only entries of chunks that hold
  *                one of the sequence's lens[b] tokens are read; the others may hold anything
  *   lens         device int32 [n_seqs]: tokens of sequence b in the cache, 0 .. max_len (0: an empty row of the batch)
@@ -303,7 +303,7 @@ typedef enum llms_dtype { LLMS_F16 = 0, LLMS_BF16 = 1 } llms_dtype;
  *             multiple of 8
  *   k_new, v_new  device [n_seqs] rows of n_kv_heads * head_dim elements, new_stride elements apart (aligned like q), or
  *             both NULL.  If given, they are K and V of the newest token, t = lens[b] - 1: the call stores them in the
- *             pool and uses them.  A slot that holds a newest token must then not be listed by another sequence
+ *             pool and uses them.  A slot that holds a newest token must then not be listed anywhere else
  *   window    0: every cached token is seen, else the last `window` ones
  *   out       device [n_seqs][n_q_heads][head_dim], 16-byte aligned
  *   lse       device fp32 [n_seqs][n_q_heads], or NULL
@@ -312,8 +312,9 @@ typedef enum llms_dtype { LLMS_F16 = 0, LLMS_BF16 = 1 } llms_dtype;
  *             Entries of mass_out from lens[b] on are left as they were
  *   workspace device, 256-byte aligned, llms_decode_workspace_bytes(desc, n_seqs, max_len, mass_out != NULL); may be
  *             reused by the next call on the same stream
- * A sequence whose length is outside 0 .. max_len, or that lists a slot outside the pool, gets NaN in out and lse; nothing
- * outside the pool is read or written. */
+ * A sequence whose length is outside 0 .. max_len, or one of whose tokens' slots (those in the window) lies outside the pool,
+ * gets NaN in out and lse; nothing outside the pool is read or written.  Of an invalid length mass_out is left as it was; with
+ * a slot outside the pool the masses of the tokens in the window become NaN, as they do for a row with a NaN logit. */
 int llms_decode_workspace_bytes(const llms_kv_desc *desc, int n_seqs, int max_len, int with_mass, uint64_t *nbytes);
 int llms_decode_attention(const llms_kv_desc *desc, int dtype, int layer, void *kv, const void *q, int64_t q_stride,
                           const void *k_new, const void *v_new, int64_t new_stride, const int32_t *chunk_table,

@@ -1075,7 +1075,9 @@ static int launch_decode(DecodeArgs &a, int item_ctas, const CUtensorMap &map, c
 constexpr int kItemRounds = 2;
 static int decode_item_ctas(const DecodeArgs &a, int blocks_of_64)
 {
-    constexpr int kPerSm[4] = {3, 3, 2, 1};                   // CTAs that an SM has room for, by blocks of 64 channels
+    // CTAs that an SM has room for with up to four query rows, by blocks of 64 channels.  Rows take shared memory too: of 16 rows of
+    // 64 channels and of 8 or 16 of 128 two fit, of 8 or 16 of 192 one, so that their rounds may be more than kItemRounds
+    constexpr int kPerSm[4] = {3, 3, 2, 1};
     if (a.mass_out && a.blocks > 1) return 0;                 // a token's weight is made of several items' logits
     const int seen = a.window > 0 ? (int)std::min<int64_t>(a.max_len, (int64_t)a.window + kTile - 1) : a.max_len, tiles = (seen + kTile - 1) / kTile;
     const int64_t n_items = (int64_t)a.n_seqs * a.Hkv * a.blocks, room = (int64_t)sm_count() * kPerSm[blocks_of_64 - 1] * kItemRounds;

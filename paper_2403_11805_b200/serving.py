@@ -3,8 +3,12 @@
 A Serving is a batch of contexts whose working sets are locked in the pool: their chunk table and lengths on the device, an
 accumulator of attention weights per layer, KV head and token, and the calls that a decoding step makes.  A model
 calls `decode` once per layer with the step's query, key and value rows; `shrink` drops the tokens that attention weighed
-least and gives the slots they no longer need back to the pool.  Lengths follow rules that the host knows as well
-(one more token a step, min(budget, length) after a shrink), so nothing here waits for the device.
+least and gives the slots they no longer need back to the pool.  The accumulator belongs to the batch: it starts at zero, so
+`shrink` ranks by what the `decode` calls of this step have added (of tokens with equal weight the first stay).
+
+Lengths follow rules that the host knows as well (one more token a step, min(budget, length) after a shrink), so no length is
+read back from the device.  `decode` and an `advance` within the last chunk wait for nothing; growth into a new chunk and
+`shrink` copy the changed table from pageable memory, which waits for the stream.
 
 The calls run on the pool's stream, in order with its Reclaim and Load.  Made on another stream they come after what was queued
 there, and what is queued there next comes after them.  Only a `decode` that is being captured into a graph stays on the
