@@ -46,8 +46,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Weights are taken against a reference that follows the running maximum in steps: it moves only when a logit exceeds it by more
 // than kSlack (in units of log2), so most tiles need no maximum over the warp's lanes and no rescaling.
 // For the product with V a weight goes into the MMA as kLift times its value, as a sum of two 16-bit values hi + lo.  hi is cut
-// off a little below the weight, so that lo is never 0: a value of V that is infinite then gives an infinity, not 0 * inf.  The
-// lift (a power of two, taken back exactly at the end) keeps kLift * 2^kSlack in fp16's range.  hi + lo is off by less than
+// off a little below the weight, so that lo is not 0 (of weights above 2^-30 of the reference in fp16, of any that is not 0 in bf16):
+// a value of V that is infinite then gives an infinity, not 0 * inf.  The lift (a power of two, taken back exactly at the end) keeps kLift * 2^kSlack in fp16's range.  hi + lo is off by less than
 // 2^-20 (fp16) or 2^-15.6 (bf16) of the weight; one 16-bit value alone would add an error as large as the rounding of the
 // output itself.  fp16's smallest step makes it 2^-31 of the reference at least: weights below 2^-11 of it have fewer bits, those
 // below 2^-31 none (4000 of them together less than half a step of an fp16 output next to values of its size).

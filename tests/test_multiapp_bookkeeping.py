@@ -290,3 +290,61 @@ def test_an_empty_step_settles_what_the_last_one_left(device):
     app.step(k=4)
     assert device.queue == [] and not app._pending
     assert all(app.checksum[r] == device.slots[int(app.slot[r])] for c in range(4) for r in app.rows(c) if app.slot[r] >= 0)
+
+
+@pytest.mark.parametrize("aot", [False, True], ids=["reclaim", "aot"])
+@pytest.mark.parametrize("seed", range(6))
+def test_random_steps_keep_every_chunk(device, seed, aot):
+    """Contexts are served, grown, shrunk, and their callbacks raise, in a pool that holds a third of them: every chunk is in its
+    slot or, with its checksum, in the arena."""
+    rng = np.random.RandomState(seed)
+    cpc, n_ctx = 7, 9
+    sh = synth.KVShape("apps", 1, 1, 1, 16, cpc * 16, 16, 16, window=4, seed=1, n_contexts=n_ctx)
+    app = multiapp.MultiApp(sh, n_slots=3 * cpc, seed=seed, aot=aot)
+    app._alloc_buffers()
+    for c in range(n_ctx):
+        bits, _ = B.assign_bits(np.arange(cpc, dtype=np.float32), app.frac)
+        app._place_in_arena(c, bits)
+    truth = {}
+    for row in range(n_ctx * cpc):
+        truth[row] = app.checksum[row] = device.arena[int(app.arena_off[row])] = device.new_content()
+
+    def change(row):
+        slot, truth[row] = int(app.slot[row]), device.new_content()
+        device.queue.append(lambda value=truth[row]: device.slots.update({slot: value}))
+
+    def serve(s):
+        held = {r: (int(app.slot[r]), truth[r]) for c in s.ctxs for r in app.rows(c)}
+        device.wait()
+        assert all(device.slots[slot] == value for slot, value in held.values())
+        for _ in range(rng.randint(0, 60)):
+            if rng.rand() < 0.15:
+                s.shrink(int(rng.randint(1, cpc * 16)), 1)
+                for i, c in enumerate(s.ctxs):
+                    for r in range(c * cpc, c * cpc + -(-int(s.lengths[i]) // 16)):
+                        change(r)
+            elif (s.lengths < s.capacity).all():
+                s.advance()
+                for i, c in enumerate(s.ctxs):
+                    change(c * cpc + (int(s.lengths[i]) - 1) // 16)
+        if rng.rand() < 0.2:
+            raise KeyError("the model's own")
+
+    for _ in range(60):
+        try:
+            app.step(k=int(rng.randint(1, 4)), serve=serve if rng.rand() < 0.8 else None)
+        except KeyError:
+            pass
+        if rng.rand() < 0.3:
+            app.finish()
+        device.wait()
+        app._collect_checksums()
+        live = np.concatenate([app.rows(c) for c in range(n_ctx)])
+        res = np.flatnonzero(app.slot >= 0)
+        assert set(res) <= set(live) and not app.table["locked"].any() and np.array_equal(app.slot >= 0, app.table["resident"] != 0)
+        assert sorted([int(x) for x in app.slot[res]] + app.free) == list(range(app.n_slots))
+        for r in live:
+            if app.slot[r] >= 0:
+                assert device.slots[int(app.slot[r])] == truth[r]
+            if app.slot[r] < 0 or app.clean[r]:
+                assert device.arena[int(app.arena_off[r])] == truth[r] == app.checksum[r]
