@@ -343,6 +343,64 @@ int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float *mass, int
                       int budget, int recent, const int32_t *dst_table, int dst_stride, float *mass_out,
                       int32_t *kept, int32_t *new_lens, void *stream);
 
+/* ------------------------------------------------------------------ a cache held at 8 or 4 bits */
+
+/* A second kind of pool, for contexts that stay resident at few bits: K and V are quantised token by token as they are written,
+ * by the rule of the swap records (a group is group_size channels of one token of one KV head; see the record format above),
+ * and attention reads the codes.  `desc` gives the pool's shape as above (n_tokens = slots * chunk_len; quant_mode 0; the strides are
+ * checked but have no influence) and `bits` (4 or 8) the width of its codes.  A held pool is llms_held_bytes(desc, bits) bytes,
+ *     [n_layers][n_kv_heads][tile][K codes | V codes | K parameters | V parameters],
+ * a tile being 16 consecutive rows of the pool.  Parameters: [token][group] of {u16 scale, u16 zero-point} (fp16 bits).  With
+ * W = head_dim * bits / 128 and VW the largest of 4, 2, 1 that divides W, K codes of a token are 4 W little-endian words of 32 bits
+ * (channels in order from the lowest bit on), word 4 w + j of token 8 i + g lying at place [i][w / VW][g][j][w % VW]; V codes of a
+ * token are 8 W units of 16 bits, unit 8 w + g of token 8 i + 2 j + e at place [i][w / VW][g][j][w % VW][e]  (i, e < 2; g < 8; j < 4).
+ * Rows of fp16 are quantised as they are, rows of bf16 after rounding to fp16 (values beyond 65504 as +-65504).  A group with an
+ * infinity or a NaN is held as codes 0, scale 0 and a NaN zero-point: all its values are NaN.
+ * Batches, chunk tables, lens and max_len are as for the calls above.
+ * Needed: head_dim 64, 96, 128 or 256; group_size 32 or more, a power of two, with at most four groups per row; chunk_len a multiple of
+ * 16; the limits of the calls above (LLMS_ERR_UNSUPPORTED otherwise; bits of 1 and 2 too). */
+int llms_held_bytes(const llms_kv_desc *desc, int bits, uint64_t *nbytes);
+
+/* Quantises K and V rows of new tokens into the pool, one layer.
+ *   dtype     type of the rows (llms_dtype)
+ *   held      device, the pool, 16-byte aligned
+ *   k, v      device, n_rows rows of n_kv_heads * head_dim elements, row_stride elements apart; 16-byte aligned, row_stride a
+ *             multiple of 8
+ *   first_row device int32 [n_seqs + 1], ascending: rows first_row[b] .. first_row[b + 1] - 1 are the last tokens of sequence b,
+ *             in order (the last row is token lens[b] - 1).  Rows before the first sequence's or behind the last one's are
+ *             nobody's.  NULL: row b is the newest token of sequence b (n_rows == n_seqs; of an empty sequence it is nobody's)
+ *   lens      tokens of the sequences, the new ones included
+ *   k_seen, v_seen  device, rows like k and v (seen_stride apart), or both NULL: the values that the pool now holds, rounded to the
+ *             rows' type (fp16: saturated): what attention over the pool sees of these tokens.  May be k and v themselves.
+ *             Nobody's rows are left as they were
+ * Codes and parameters of all other tokens stay as they are.  A slot that gets new tokens must not be listed anywhere else.  Rows of a
+ * sequence whose length is outside 0 .. max_len, or that has more rows than tokens, and of tokens whose slot lies outside the
+ * pool are not stored; their seen rows are NaN. */
+int llms_held_write(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, const void *k, const void *v,
+                    int64_t row_stride, int n_rows, const int32_t *first_row, const int32_t *chunk_table, int table_stride,
+                    const int32_t *lens, int n_seqs, int max_len, void *k_seen, void *v_seen, int64_t seen_stride, void *stream);
+
+/* The way back: rows first_row[b] .. first_row[b + 1] - 1 of k_out and v_out get the values held of the last tokens of sequence b
+ * (of its first m tokens where lens[b] is given as m), in the rows' type.  Arguments, nobody's rows and what becomes NaN as in
+ * llms_held_write. */
+int llms_held_read(const llms_kv_desc *desc, int bits, int dtype, int layer, const void *held, const int32_t *chunk_table,
+                   int table_stride, const int32_t *lens, int n_seqs, int max_len, const int32_t *first_row, int n_rows,
+                   void *k_out, void *v_out, int64_t out_stride, void *stream);
+
+/* llms_decode_attention over a held pool: one new token per sequence attends to its tokens' held values (zero-point + code * scale,
+ * unrounded), one layer.  k_new and v_new, if given, are quantised into the pool as token lens[b] - 1 by the same call, which then
+ * sees them as they are held.  Sums are kept in binary32.  All arguments and results as there, without masses; dtype is that of
+ * q, k_new, v_new and out.  A query row with an infinity or a NaN gives NaN.
+ * The products with V take a token's weight times its scale as a pair of 16-bit values: off by less than 2^-20 of it, and by up to
+ * 2^-29 of the row's largest weight times its largest scale, which smaller products lose.
+ *   workspace device, 256-byte aligned, llms_held_workspace_bytes(desc, bits, n_seqs, max_len); may be reused by the next call on the
+ *             same stream */
+int llms_held_workspace_bytes(const llms_kv_desc *desc, int bits, int n_seqs, int max_len, uint64_t *nbytes);
+int llms_held_attention(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, const void *q, int64_t q_stride,
+                        const void *k_new, const void *v_new, int64_t new_stride, const int32_t *chunk_table, int table_stride,
+                        const int32_t *lens, int n_seqs, int max_len, int window, float scale, void *out, float *lse,
+                        void *workspace, uint64_t workspace_bytes, void *stream);
+
 /* ------------------------------------------------------------------ swap copies */
 
 /* Copy n records between a device swap buffer and a pinned host arena on `side_stream`
