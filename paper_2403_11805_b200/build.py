@@ -57,7 +57,7 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
     jobs = [(src, "", []) for src in sources()]
     if debug_bounds:
         jobs.append((os.path.join(CSRC, "codec.cu"), "_debug", ["-DLLMS_DEBUG_BOUNDS"]))
-    with ThreadPoolExecutor(max_workers=6) as pool:
+    with ThreadPoolExecutor(max_workers=8) as pool:
         objects = list(pool.map(compile_one, jobs))
     plain = objects[:len(sources())]
     link = [nvcc_path(), "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o"]
