@@ -46,7 +46,7 @@ struct DecodeArgs {
     int table_stride, n_seqs, max_len, window, Hkv, Hq, group, d, chunk_len, n_slots;
     int blocks;                                   // blocks of query rows per KV head
     int piece_shift;                              // log2 of the tokens per TMA box: the largest power of two up to 16 that divides chunk_len
-    Divisor by_chunk, by_blocks, by_per_seq, by_mass_x, by_hkv;
+    Divisor by_chunk, by_blocks, by_per_seq, by_mass_x, by_hkv, by_group;
     int rows;                                     // query rows kept per partial result
     int runs, grid_runs, few_tiles;               // runs; runs at most (CTAs of the main kernel), which up to few_tiles tiles are cut into
     int q_bytes;                                  // of an item's query rows
@@ -59,13 +59,14 @@ struct DecodeArgs {
 struct SeqTiles {
     int len, first, tile0, n;                     // tokens; first token seen; its tile; tiles (0 for an empty or invalid row)
 };
+template <int TILE = kTile>
 __device__ __forceinline__ SeqTiles seq_tiles(const DecodeArgs &a, int len)
 {
     SeqTiles s;
     s.len = len < 0 || len > a.max_len ? 0 : len;
     s.first = a.window > 0 && s.len > a.window ? s.len - a.window : 0;
-    s.tile0 = s.first / kTile;
-    s.n = (s.len + kTile - 1) / kTile - s.tile0;
+    s.tile0 = s.first / TILE;
+    s.n = (s.len + TILE - 1) / TILE - s.tile0;
     return s;
 }
 
@@ -548,7 +549,7 @@ struct DecodeLayout {
 };
 
 // warps: per SM, as many as it takes to keep the memory busy
-inline DecodeLayout decode_layout(const llms_kv_desc &d, int n_seqs, int max_len, bool with_mass, int warps)
+inline DecodeLayout decode_layout(const llms_kv_desc &d, int n_seqs, int max_len, bool with_mass, int warps, int tile = kTile)
 {
     DecodeLayout t;
     const int group = d.n_q_heads / d.n_kv_heads;
@@ -561,7 +562,7 @@ inline DecodeLayout decode_layout(const llms_kv_desc &d, int n_seqs, int max_len
     // slower), or a small multiple of that where a run then still has kRunTiles tiles: the warps that get done early take
     // the next ones.  A batch of many items whose tiles come to less than six a run is cut finer (few items: their many
     // pieces would cost more in finish_kernel).  max_len is a bound; the device knows better (struct Runs)
-    const uint64_t most_tiles = (uint64_t)n_seqs * d.n_kv_heads * t.blocks * (((uint64_t)max_len + kTile - 1) / kTile);
+    const uint64_t most_tiles = (uint64_t)n_seqs * d.n_kv_heads * t.blocks * (((uint64_t)max_len + tile - 1) / tile);
     const uint64_t room = (uint64_t)sm_count() * warps;
     const uint64_t rounds = std::min<uint64_t>(kRounds, std::max<uint64_t>(1, most_tiles / (room * kRunTiles)));
     const uint64_t finest = std::max<uint64_t>(1, most_tiles / kMinTiles);
@@ -591,6 +592,7 @@ inline void set_decode_shape(DecodeArgs &a, const llms_kv_desc &d, const DecodeL
     a.by_blocks = Divisor(a.blocks);
     a.by_per_seq = Divisor(a.Hkv * a.blocks);
     a.by_hkv = Divisor(a.Hkv);
+    a.by_group = Divisor(a.group);
     a.scale_log2 = scale * kLog2e;
     a.runs = lay.runs; a.grid_runs = lay.grid_runs; a.few_tiles = lay.few_tiles;
     a.q_bytes = a.rows * a.d * 2;
@@ -600,14 +602,14 @@ inline void set_decode_shape(DecodeArgs &a, const llms_kv_desc &d, const DecodeL
 // GPU (per_sm: CTAs that an SM has room for); not if a warp is left with more than four tiles, in a batch (whose sequences are
 // seldom all as long as max_len) eight.
 constexpr int kItemRounds = 2;
-inline int decode_item_ctas(const DecodeArgs &a, int per_sm)
+inline int decode_item_ctas(const DecodeArgs &a, int per_sm, int rounds = kItemRounds, int tile = kTile, int warps = kItemWarps)
 {
     if (a.mass_out && a.blocks > 1) return 0;                 // a token's weight is made of several items' logits
-    const int seen = a.window > 0 ? (int)std::min<int64_t>(a.max_len, (int64_t)a.window + kTile - 1) : a.max_len, tiles = (seen + kTile - 1) / kTile;
-    const int64_t n_items = (int64_t)a.n_seqs * a.Hkv * a.blocks, room = (int64_t)sm_count() * per_sm * kItemRounds;
+    const int seen = a.window > 0 ? (int)std::min<int64_t>(a.max_len, (int64_t)a.window + tile - 1) : a.max_len, tiles = (seen + tile - 1) / tile;
+    const int64_t n_items = (int64_t)a.n_seqs * a.Hkv * a.blocks, room = (int64_t)sm_count() * per_sm * rounds;
     int ctas = 1;
-    while (ctas < 8 && ctas * kItemWarps < tiles && n_items * ctas * 2 <= room) ctas *= 2;
-    return n_items * ctas <= room && tiles <= ctas * kItemWarps * (a.n_seqs > 1 ? 8 : 4) ? ctas : 0;
+    while (ctas < 8 && ctas * warps < tiles && n_items * ctas * 2 <= room) ctas *= 2;
+    return n_items * ctas <= room && tiles <= ctas * warps * (a.n_seqs > 1 ? 8 : 4) ? ctas : 0;
 }
 
 }  // namespace llms

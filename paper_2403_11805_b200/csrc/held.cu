@@ -328,11 +328,14 @@ int check_held(const llms_kv_desc *d, int bits, int n_seqs, int max_len)
 {
     const int rc = check_paged(d, n_seqs, max_len);
     if (rc) return rc;
+    if (n_chunks(*d) < 1) return LLMS_ERR_INVALID_ARG;
+    if (max_len > 0x7fffff00) return LLMS_ERR_UNSUPPORTED;    // positions are counted up to a tile further, in 32 bits
     if (check_bits(bits)) return LLMS_ERR_BAD_BITS;
     if (bits != 4 && bits != 8) return LLMS_ERR_UNSUPPORTED;
     if (d->quant_mode != 0 || d->chunk_len % 16) return LLMS_ERR_UNSUPPORTED;
     if (d->head_dim != 64 && d->head_dim != 96 && d->head_dim != 128 && d->head_dim != 256) return LLMS_ERR_UNSUPPORTED;
     if (d->group_size < 32 || !is_pow2(d->group_size) || d->head_dim / d->group_size > 4) return LLMS_ERR_UNSUPPORTED;
+    if ((int64_t)d->n_kv_heads * held_tiles(*d) > 0x7fffffff) return LLMS_ERR_UNSUPPORTED;       // a layer's tiles are numbered in 32 bits
     return LLMS_OK;
 }
 
