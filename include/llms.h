@@ -363,7 +363,8 @@ int llms_held_bytes(const llms_kv_desc *desc, int bits, uint64_t *nbytes);
 
 /* Quantises K and V rows of new tokens into the pool, one layer.
  *   dtype     type of the rows (llms_dtype)
- *   held      device, the pool, 16-byte aligned
+ *   held      device, the pool, 16-byte aligned, held_size bytes long (LLMS_ERR_BUF_TOO_SMALL if that is less than
+ *             llms_held_bytes)
  *   k, v      device, n_rows rows of n_kv_heads * head_dim elements, row_stride elements apart; 16-byte aligned, row_stride a
  *             multiple of 8
  *   first_row device int32 [n_seqs + 1], ascending: rows first_row[b] .. first_row[b + 1] - 1 are the last tokens of sequence b,
@@ -376,15 +377,15 @@ int llms_held_bytes(const llms_kv_desc *desc, int bits, uint64_t *nbytes);
  * Codes and parameters of all other tokens stay as they are.  A slot that gets new tokens must not be listed anywhere else.  Rows of a
  * sequence whose length is outside 0 .. max_len, or that has more rows than tokens, and of tokens whose slot lies outside the
  * pool are not stored; their seen rows are NaN. */
-int llms_held_write(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, const void *k, const void *v,
-                    int64_t row_stride, int n_rows, const int32_t *first_row, const int32_t *chunk_table, int table_stride,
+int llms_held_write(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, uint64_t held_size, const void *k,
+                    const void *v, int64_t row_stride, int n_rows, const int32_t *first_row, const int32_t *chunk_table, int table_stride,
                     const int32_t *lens, int n_seqs, int max_len, void *k_seen, void *v_seen, int64_t seen_stride, void *stream);
 
 /* The way back: rows first_row[b] .. first_row[b + 1] - 1 of k_out and v_out get the values held of the last tokens of sequence b
  * (of its first m tokens where lens[b] is given as m), in the rows' type.  Arguments, nobody's rows and what becomes NaN as in
  * llms_held_write. */
-int llms_held_read(const llms_kv_desc *desc, int bits, int dtype, int layer, const void *held, const int32_t *chunk_table,
-                   int table_stride, const int32_t *lens, int n_seqs, int max_len, const int32_t *first_row, int n_rows,
+int llms_held_read(const llms_kv_desc *desc, int bits, int dtype, int layer, const void *held, uint64_t held_size,
+                   const int32_t *chunk_table, int table_stride, const int32_t *lens, int n_seqs, int max_len, const int32_t *first_row, int n_rows,
                    void *k_out, void *v_out, int64_t out_stride, void *stream);
 
 /* llms_decode_attention over a held pool: one new token per sequence attends to its tokens' held values (zero-point + code * scale,
@@ -396,8 +397,8 @@ int llms_held_read(const llms_kv_desc *desc, int bits, int dtype, int layer, con
  *   workspace device, 256-byte aligned, llms_held_workspace_bytes(desc, bits, n_seqs, max_len); may be reused by the next call on the
  *             same stream */
 int llms_held_workspace_bytes(const llms_kv_desc *desc, int bits, int n_seqs, int max_len, uint64_t *nbytes);
-int llms_held_attention(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, const void *q, int64_t q_stride,
-                        const void *k_new, const void *v_new, int64_t new_stride, const int32_t *chunk_table, int table_stride,
+int llms_held_attention(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, uint64_t held_size, const void *q,
+                        int64_t q_stride, const void *k_new, const void *v_new, int64_t new_stride, const int32_t *chunk_table, int table_stride,
                         const int32_t *lens, int n_seqs, int max_len, int window, float scale, void *out, float *lse,
                         void *workspace, uint64_t workspace_bytes, void *stream);
 

@@ -77,12 +77,12 @@ _SIGNATURES = {
                                     C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.c_void_p]),
     "llms_held_bytes": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p]),
-    "llms_held_write": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_void_p,
+    "llms_held_write": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_void_p,
                                   C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
-    "llms_held_read": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int,
+    "llms_held_read": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int,
                                  C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "llms_held_workspace_bytes": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p]),
-    "llms_held_attention": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+    "llms_held_attention": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_uint64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
                                       C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_float, C.c_void_p,
                                       C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
     "llms_lctru_order": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p]),
@@ -533,75 +533,75 @@ def held_workspace_bytes(desc, bits, n_seqs, max_len):
     return nb.value
 
 
-def _check_held(what, device, desc, bits, layer, held, table, lens, max_len):
-    """The pool and the batch of a call on a held pool: how far apart the table's rows lie."""
-    if not (_is_batch(table, lens, device) and held.get_device() == device and held.is_contiguous()):
-        _refuse(what, device, f"a contiguous pool, chunk_table int32 [{lens.shape[0] if lens.dim() else 0}, chunks] and lens int32 [sequences] on this device",
-                held=held, chunk_table=table, lens=lens)
+def _refuse_held(what, device, desc, held, table, lens, max_len, numbers):
+    """What is wrong with the pool or the batch of a call on a held pool."""
+    if not (table.dim() == 2 and lens.dim() == 1 and _is_batch(table, lens, device) and held.get_device() == device and held.is_contiguous()):
+        _refuse(what, device, "a contiguous pool, chunk_table int32 [sequences, chunks] and lens int32 [sequences] on this device", held=held,
+                chunk_table=table, lens=lens)
     if table.shape[1] * desc.chunk_len < max_len:
         _refuse(what, device, f"max_len {max_len} is more than a table row's chunks of {desc.chunk_len} hold", chunk_table=table)
-    if (layer | bits) >> 31:                                  # negative, or not an int of the C call
-        _refuse(what, device, f"layer {layer}, bits {bits}")
-    if held.nbytes < _held_size(desc, bits):
-        raise LlmsError(ERR_BUF_TOO_SMALL, f"{what}: a held pool of {held.nbytes} bytes, {_held_size(desc, bits)} are needed")
-    return table.stride(0) if lens.shape[0] > 1 else table.shape[1]
+    _refuse(what, device, "negative, or not an int of the C call: " + ", ".join(f"{k} {v}" for k, v in numbers.items()))
 
 
-def _held_size(desc, bits):
-    """held_bytes, without the call into the library where the descriptor was seen before."""
-    known = getattr(desc, "_held_size", None)
-    shape = (bits, desc.n_layers, desc.n_kv_heads, desc.head_dim, desc.n_tokens, desc.chunk_len, desc.group_size, desc.quant_mode)
-    if known is None or known[0] != shape:
-        known = desc._held_size = (shape, held_bytes(desc, bits))
-    return known[1]
+def _refuse_rows(what, device, names, heads, d, k, v):
+    _refuse(what, device, f"{names} together, [rows, {heads}, {d}] of one type, a row's heads side by side, both with the same strides", k=k, v=v)
 
 
-def _row_pair(what, device, names, k, v, heads, d, dtype, rows=None):
-    """Two arrays of rows [rows, heads, d], side by side in the same way: how far apart the rows lie."""
-    n = k.shape[0] if rows is None and k.dim() == 3 else rows
-    strides = k.stride()
-    if not (k.shape == (n, heads, d) == v.shape and k.dtype is dtype and v.dtype is dtype and k.get_device() == device and v.get_device() == device
-            and (n == 0 or (strides[2] == 1 and (strides[1] == d or heads == 1) and (strides == v.stride() or (n == 1 and v.is_contiguous()))))):
-        _refuse(what, device, f"{names} [rows, {heads}, {d}] of {dtype}, a row's heads side by side, both with the same strides", k=k, v=v)
-    return strides[0] if n > 1 else heads * d
-
-
-def _first_row(what, device, first_row, n_seqs, n_rows):
-    if first_row is None:
-        if n_rows != n_seqs:
-            _refuse(what, device, f"{n_rows} rows for {n_seqs} sequences: first_row says whose they are")
+def _row_stride(k, v, n, heads, d, dtype, device):
+    """How far apart the rows of two arrays [n, heads, d] lie, or None if they do not lie alike."""
+    if k is None or v is None or k.shape != (n, heads, d) or v.shape != (n, heads, d) or k.dtype is not dtype or v.dtype is not dtype \
+            or k.get_device() != device or v.get_device() != device:
         return None
-    if not _is_whole(first_row, (n_seqs + 1,), _torch.int32, device):
-        _refuse(what, device, f"first_row int32 [{n_seqs + 1}]", first_row=first_row)
-    return first_row.data_ptr()
+    row, head, channel = k.stride()
+    if n > 1:
+        return row if channel == 1 and (head == d or heads == 1) and v.stride() == (row, head, channel) else None
+    return heads * d if n == 0 or (channel == 1 and (head == d or heads == 1) and (v.stride(2) == 1 and (v.stride(1) == d or heads == 1))) else None
+
+
+def _held_rows(what, desc, bits, layer, held, table, lens, max_len, k, v, names, first_row, stream):
+    """What a write and a read have in common."""
+    device, stream = _current(stream)
+    dtype, heads, d, i32 = k.dtype, desc.n_kv_heads, desc.head_dim, _torch.int32
+    code = _CACHE_TYPES.get(dtype)
+    if code is None:
+        raise LlmsError(ERR_UNSUPPORTED, f"{what}: rows of {dtype} (float16 and bfloat16 are taken)")
+    if not (lens.dtype is i32 and lens.dim() == 1 and table.dim() == 2 and table.dtype is i32 and lens.get_device() == device
+            and table.get_device() == device and held.get_device() == device and lens.is_contiguous() and held.is_contiguous()):
+        _refuse_held(what, device, desc, held, table, lens, max_len, {})
+    n, (seqs, chunks), (table_stride, entry) = lens.shape[0], table.shape, table.stride()
+    if seqs != n or (entry != 1 and chunks != 1) or chunks * desc.chunk_len < max_len or (layer | bits | max_len) >> 31:
+        _refuse_held(what, device, desc, held, table, lens, max_len, dict(layer=layer, bits=bits, max_len=max_len))
+    rows = k.shape[0]
+    stride = _row_stride(k, v, rows, heads, d, dtype, device)
+    if stride is None:
+        _refuse_rows(what, device, names, heads, d, k, v)
+    if first_row is None:
+        if rows != n:
+            _refuse(what, device, f"{rows} rows for {n} sequences: first_row says whose they are")
+    elif not (first_row.shape == (n + 1,) and first_row.dtype is i32 and first_row.get_device() == device and first_row.is_contiguous()):
+        _refuse(what, device, f"first_row int32 [{n + 1}]", first_row=first_row)
+    return device, stream, code, n, rows, stride, table_stride if n > 1 else chunks, None if first_row is None else first_row.data_ptr()
 
 
 def held_write(desc, bits, layer, held, k, v, chunk_table, lens, max_len, first_row=None, k_seen=None, v_seen=None, stream=None):
     """llms_held_write: K and V rows of new tokens are quantised into one layer of a held pool.
-    held: uint8, held_bytes(desc, bits) of them; k, v: [rows, n_kv_heads, head_dim] (fp16 or bf16, views of one projection's output will
+    held: held_bytes(desc, bits) bytes; k, v: [rows, n_kv_heads, head_dim] (fp16 or bf16, views of one projection's output will
     do); chunk_table: int32 [n_seqs, chunks]; lens: int32 [n_seqs], the new tokens included; first_row: int32 [n_seqs + 1], sequence
     b's rows begin there (None: one row per sequence); k_seen, v_seen: like k and v, get the values that are held.  All tensors on
     the current device."""
     what = "llms_held_write"
-    device, stream = _current(stream)
-    dtype, n, hk, d = k.dtype, lens.shape[0] if lens.dim() else 0, desc.n_kv_heads, desc.head_dim
-    code = _CACHE_TYPES.get(dtype)
-    if code is None:
-        raise LlmsError(ERR_UNSUPPORTED, f"{what}: rows of {dtype} (float16 and bfloat16 are taken)")
-    table_stride = _check_held(what, device, desc, bits, layer, held, chunk_table, lens, max_len)
-    stride = _row_pair(what, device, "k and v", k, v, hk, d, dtype)
-    rows = k.shape[0]
+    device, stream, code, n, rows, stride, table_stride, first = _held_rows(what, desc, bits, layer, held, chunk_table, lens, max_len, k, v, "k and v",
+                                                                            first_row, stream)
     k_ptr = v_ptr = None
     seen_stride = 0
     if k_seen is not None or v_seen is not None:
-        if k_seen is None or v_seen is None:
-            _refuse(what, device, "k_seen and v_seen together", k_seen=k_seen, v_seen=v_seen)
-        seen_stride = _row_pair(what, device, "k_seen and v_seen", k_seen, v_seen, hk, d, dtype, rows)
+        seen_stride = _row_stride(k_seen, v_seen, rows, desc.n_kv_heads, desc.head_dim, k.dtype, device)
+        if seen_stride is None:
+            _refuse_rows(what, device, "k_seen and v_seen like k and v,", desc.n_kv_heads, desc.head_dim, k_seen, v_seen)
         k_ptr, v_ptr = k_seen.data_ptr(), v_seen.data_ptr()
     rc = (_lib or lib()).llms_held_write(
-        C.addressof(desc), bits, code, layer, held.data_ptr(), k.data_ptr(), v.data_ptr(), stride, rows,
-        _first_row(what, device, first_row, n, rows), chunk_table.data_ptr(), table_stride, lens.data_ptr(), n, max_len, k_ptr, v_ptr,
-        seen_stride, stream)
+        C.addressof(desc), bits, code, layer, held.data_ptr(), held.nbytes, k.data_ptr(), v.data_ptr(), stride, rows, first,
+        chunk_table.data_ptr(), table_stride, lens.data_ptr(), n, max_len, k_ptr, v_ptr, seen_stride, stream)
     if rc < 0:
         raise LlmsError(rc, what)
 
@@ -610,17 +610,11 @@ def held_read(desc, bits, layer, held, chunk_table, lens, max_len, k_out, v_out,
     """llms_held_read: the values held of the sequences' last tokens, as rows k_out, v_out [rows, n_kv_heads, head_dim] (fp16 or bf16);
     everything else as in held_write."""
     what = "llms_held_read"
-    device, stream = _current(stream)
-    dtype, n = k_out.dtype, lens.shape[0] if lens.dim() else 0
-    code = _CACHE_TYPES.get(dtype)
-    if code is None:
-        raise LlmsError(ERR_UNSUPPORTED, f"{what}: rows of {dtype} (float16 and bfloat16 are taken)")
-    table_stride = _check_held(what, device, desc, bits, layer, held, chunk_table, lens, max_len)
-    stride = _row_pair(what, device, "k_out and v_out", k_out, v_out, desc.n_kv_heads, desc.head_dim, dtype)
-    rows = k_out.shape[0]
+    _, stream, code, n, rows, stride, table_stride, first = _held_rows(what, desc, bits, layer, held, chunk_table, lens, max_len, k_out, v_out,
+                                                                       "k_out and v_out", first_row, stream)
     rc = (_lib or lib()).llms_held_read(
-        C.addressof(desc), bits, code, layer, held.data_ptr(), chunk_table.data_ptr(), table_stride, lens.data_ptr(), n, max_len,
-        _first_row(what, device, first_row, n, rows), rows, k_out.data_ptr(), v_out.data_ptr(), stride, stream)
+        C.addressof(desc), bits, code, layer, held.data_ptr(), held.nbytes, chunk_table.data_ptr(), table_stride, lens.data_ptr(), n, max_len,
+        first, rows, k_out.data_ptr(), v_out.data_ptr(), stride, stream)
     if rc < 0:
         raise LlmsError(rc, what)
 
@@ -628,34 +622,38 @@ def held_read(desc, bits, layer, held, chunk_table, lens, max_len, k_out, v_out,
 def held_attention(desc, bits, layer, held, q, chunk_table, lens, max_len, out, workspace, k_new=None, v_new=None, window=0, scale=None,
                    lse=None, stream=None):
     """llms_held_attention: one new token per sequence attends to its tokens in one layer of a held pool.
-    held: uint8, held_bytes(desc, bits) of them; q, out: [n_seqs, n_q_heads, head_dim] (fp16 or bf16); k_new, v_new: [n_seqs, n_kv_heads,
+    held: held_bytes(desc, bits) bytes; q, out: [n_seqs, n_q_heads, head_dim] (fp16 or bf16); k_new, v_new: [n_seqs, n_kv_heads,
     head_dim], quantised into the pool at position lens - 1; everything else as in decode_attention."""
     what = "llms_held_attention"
     device, stream = _current(stream)
-    dtype, n, d, hq = q.dtype, lens.shape[0] if lens.dim() else 0, desc.head_dim, desc.n_q_heads
+    dtype, d, hq, i32 = q.dtype, desc.head_dim, desc.n_q_heads, _torch.int32
     code = _CACHE_TYPES.get(dtype)
     if code is None:
         raise LlmsError(ERR_UNSUPPORTED, f"{what}: rows of {dtype} (float16 and bfloat16 are taken)")
-    table_stride = _check_held(what, device, desc, bits, layer, held, chunk_table, lens, max_len)
+    if not (lens.dtype is i32 and lens.dim() == 1 and chunk_table.dim() == 2 and chunk_table.dtype is i32 and lens.get_device() == device
+            and chunk_table.get_device() == device and held.get_device() == device and lens.is_contiguous() and held.is_contiguous()):
+        _refuse_held(what, device, desc, held, chunk_table, lens, max_len, {})
+    n, (seqs, chunks), (table_stride, entry) = lens.shape[0], chunk_table.shape, chunk_table.stride()
+    if seqs != n or (entry != 1 and chunks != 1) or chunks * desc.chunk_len < max_len or (layer | bits | max_len | window) >> 31:
+        _refuse_held(what, device, desc, held, chunk_table, lens, max_len, dict(layer=layer, bits=bits, max_len=max_len, window=window))
     q_stride, q_head, q_channel = q.stride() if q.dim() == 3 else (0, 0, 0)
     if not (q.shape == (n, hq, d) and q.get_device() == device and q_channel == 1 and (q_head == d or hq == 1)
-            and _is_whole(out, (n, hq, d), dtype, device) and (lse is None or _is_whole(lse, (n, hq), _torch.float32, device))
+            and out.shape == (n, hq, d) and out.dtype is dtype and out.get_device() == device and out.is_contiguous()
+            and (lse is None or _is_whole(lse, (n, hq), _torch.float32, device))
             and workspace.get_device() == device and workspace.is_contiguous()):
         _refuse(what, device, f"q and out [{n}, {hq}, {d}] of one type, lse float32 [{n}, {hq}], a contiguous workspace on this device",
                 q=q, out=out, lse=lse, workspace=workspace)
-    if window >> 31:
-        _refuse(what, device, f"window {window}")
     k_ptr = v_ptr = None
     new_stride = 0
     if k_new is not None or v_new is not None:
-        if k_new is None or v_new is None:
-            _refuse(what, device, "k_new and v_new together", k_new=k_new, v_new=v_new)
-        new_stride = _row_pair(what, device, "k_new and v_new", k_new, v_new, desc.n_kv_heads, d, dtype, n)
+        new_stride = _row_stride(k_new, v_new, n, desc.n_kv_heads, d, dtype, device)
+        if new_stride is None:
+            _refuse_rows(what, device, "k_new and v_new", desc.n_kv_heads, d, k_new, v_new)
         k_ptr, v_ptr = k_new.data_ptr(), v_new.data_ptr()
     rc = (_lib or lib()).llms_held_attention(
-        C.addressof(desc), bits, code, layer, held.data_ptr(), q.data_ptr(), q_stride if n > 1 else hq * d, k_ptr, v_ptr, new_stride,
-        chunk_table.data_ptr(), table_stride, lens.data_ptr(), n, max_len, window, d ** -0.5 if scale is None else scale, out.data_ptr(),
-        None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, stream)
+        C.addressof(desc), bits, code, layer, held.data_ptr(), held.nbytes, q.data_ptr(), q_stride if n > 1 else hq * d, k_ptr, v_ptr, new_stride,
+        chunk_table.data_ptr(), table_stride if n > 1 else chunks, lens.data_ptr(), n, max_len, window, d ** -0.5 if scale is None else scale,
+        out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, stream)
     if rc < 0:
         raise LlmsError(rc, what)
 

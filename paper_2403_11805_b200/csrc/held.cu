@@ -6,11 +6,13 @@
 // Bound.  Every element is read and written once (2 bytes one way, b / 8 and its share of the parameters the other), with some ten
 // instructions in between: memory-bound.
 //
-// Split.  A warp takes K or V of one KV head's 16 tokens of one sequence: a tile of the pool, in whose order of codes its lanes hold the
+// Split.  A warp takes K and V of one KV head's 16 tokens of one sequence: a tile of the pool, in whose order of codes its lanes hold the
 // channels from the start, so that a whole tile is written (or read) in full vectors and nothing is exchanged but the ranges
-// of the groups.  A sequence's rows may begin and end inside a tile: the other tokens' codes in it are left as they are.
-// Neighbouring warps take the heads of the same tokens, whose rows lie side by side.
+// of the groups.  All its loads are under way before the first value is used.  A sequence's rows may begin and end inside
+// a tile: the other tokens' codes in it are left as they are.  Neighbouring warps take the heads of the same tokens, whose
+// rows lie side by side.
 #include <algorithm>
+#include <type_traits>
 
 #include "held.cuh"
 
@@ -24,6 +26,13 @@ struct HeldSpan {
     int64_t row0;                                 // row of the tile's first token, whether it has one or not
     int64_t tile;                                 // in the pool (per KV head), or -1: the tokens lie nowhere
     __device__ __forceinline__ bool has(int i) const { return i >= first && i < end; }
+    // whether one of tokens 8 i .. 8 i + 7 has a row; one with the parity e
+    __device__ __forceinline__ bool any(int i) const { return end > 8 * i && first < 8 * i + 8; }
+    __device__ __forceinline__ bool any(int i, int e) const
+    {
+        const int lo = max(first, 8 * i), n = min(end, 8 * i + 8) - lo;
+        return n > 1 || (n == 1 && (lo & 1) == e);
+    }
 };
 
 // Spans are numbered so that sequence b's begin at first_row[b] / 16 + 2 b: rows [f, f') touch at most (f' - f) / 16 + 2 tiles.
@@ -100,150 +109,177 @@ __host__ __device__ constexpr uint32_t magic_sum(int n)
     return s;
 }
 
-// N neighbouring channels (pairs x) of a token: their codes as N * BITS bits, and the values that they stand for.
-template <typename S, bool BF, int N>
+// fp32(x) + c with one rounding; x are fp16 bits.
+__device__ __forceinline__ float add_half(uint32_t x, float c)
+{
+    float d;
+    asm("add.rn.f32.f16 %0, %1, %2;" : "=f"(d) : "h"((unsigned short)x), "f"(c));
+    return d;
+}
+// fp32(x) * fp32(y) + c with one rounding; x and y are fp16 bits.
+__device__ __forceinline__ float fma_half(uint32_t x, uint32_t y, float c)
+{
+    float d;
+    asm("fma.rn.f32.f16 %0, %1, %2, %3;" : "=f"(d) : "h"((unsigned short)x), "h"((unsigned short)y), "f"(c));
+    return d;
+}
+// Two products, each rounded.
+__device__ __forceinline__ float2 mul_pair(float2 x, float2 y)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+    return d;
+}
+
+// N neighbouring channels (pairs x, fp16) of a token: their codes as N * BITS bits, and the values that they stand for.  PLAIN: every
+// group of the warp has finite values and a scale that is 0 or no subnormal number: then no code can pass the largest (the
+// scale is off by 2^-11 at most, the codes by less than half), and a scale of 0 needs no case of its own.
+template <typename S, bool BF, bool SEEN, bool PLAIN, int N>
 __device__ __forceinline__ uint32_t encode(const GroupRule &rule, const uint32_t (&x)[N / 2], uint32_t (&seen)[N / 2])
 {
     uint32_t word = 0u - magic_sum<S::BITS>(N);
 #pragma unroll
     for (int c = 0; c < N; c += 2) {
-        const float2 v = __half22float2(as_half2(x[c / 2]));
-        const float a = rule.template stepped<S::kTop>(v.x), b = rule.template stepped<S::kTop>(v.y);
-        word += (__float_as_uint(a) << (c * S::BITS)) + (__float_as_uint(b) << ((c + 1) * S::BITS));
-        seen[c / 2] = to_row<BF>(rule.value(a), rule.value(b));
+        float2 v;
+        if constexpr (PLAIN) {
+            v = mul_pair(make_float2(add_half(x[c / 2], -rule.zero), add_half(x[c / 2] >> 16, -rule.zero)), make_float2(rule.inverse, rule.inverse));
+            v.x = __fadd_rn(v.x, 12582912.0f);
+            v.y = __fadd_rn(v.y, 12582912.0f);
+        } else {
+            v = __half22float2(as_half2(x[c / 2]));
+            v.x = rule.template stepped<S::kTop>(v.x);
+            v.y = rule.template stepped<S::kTop>(v.y);
+        }
+        word += (__float_as_uint(v.x) << (c * S::BITS)) + (__float_as_uint(v.y) << ((c + 1) * S::BITS));
+        if constexpr (SEEN) seen[c / 2] = to_row<BF>(rule.value(v.x), rule.value(v.y));
     }
     return word;
 }
 
-template <typename S, bool BF>
+// The channels of one token that a lane has in words [0, W) (pairs x), which become their codes; ranges are exchanged with the
+// lanes that differ in the bits of MASK.
+template <typename S, bool BF, bool SEEN, int N, int FIRST, int LAST>
+__device__ __forceinline__ void encode_token(uint32_t (&x)[S::W][N / 2], uint32_t (&code)[S::W], bool has, bool stored, uint32_t *params, bool writes_params,
+                                             uint16_t *seen_at, int seen_step)
+{
+#pragma unroll
+    for (int grp = 0; grp < S::GPR; ++grp) {
+        GroupRange range;
+#pragma unroll
+        for (int w = grp * S::kGroupWords; w < (grp + 1) * S::kGroupWords; ++w)
+#pragma unroll
+            for (int c = 0; c < N / 2; ++c) {
+                const __half2 v = to_half2<BF>(x[w][c]);
+                x[w][c] = half2_bits(v);
+                range.add(v);
+            }
+        __half2 r = range.own();
+#pragma unroll
+        for (int d = FIRST; d < LAST; d <<= 1) r = __hmin2_nan(r, as_half2(__shfl_xor_sync(0xffffffffu, half2_bits(r), d)));
+        GroupRule rule;
+        rule.set<S::kTop>(r);
+        if (!stored) rule.zero = NAN, rule.scale = 0.0f;      // nothing is held of it
+        const bool plain = rule.zero == rule.zero && (rule.scale == 0.0f || rule.scale >= 0x1p-14f);
+        auto all_words = [&](auto is_plain) {
+#pragma unroll
+            for (int w = grp * S::kGroupWords; w < (grp + 1) * S::kGroupWords; ++w) {
+                uint32_t seen[N / 2];
+                code[w] = encode<S, BF, SEEN, decltype(is_plain)::value, N>(rule, x[w], seen);
+                if (SEEN && has) store_words(seen_at + w * seen_step, seen);
+            }
+        };
+        if (__all_sync(0xffffffffu, plain)) all_words(std::true_type());
+        else all_words(std::false_type());
+        if (writes_params) params[grp] = rule.params;
+    }
+}
+
+template <typename S, bool BF, bool SEEN>
 __global__ void __launch_bounds__(kHeldWarps * 32) held_write_kernel(const HeldRows a)
 {
     grid_dependency_wait();
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31, unit = blockIdx.x * kHeldWarps + (threadIdx.x >> 5), half = unit & 1;
-    const int span = a.by_heads(unit >> 1), h = (unit >> 1) - span * a.H;
+    const int lane = threadIdx.x & 31, unit = blockIdx.x * kHeldWarps + (threadIdx.x >> 5);
+    const int span = a.by_heads(unit), h = unit - span * a.H;
     HeldSpan s;
     if (span >= a.spans || !find_span(a, span, s)) return;
     uint8_t *tile = s.tile < 0 ? nullptr : a.held + ((int64_t)h * a.tiles + s.tile) * S::kTileBytes;
     const int g = lane >> 2, j = lane & 3;
     constexpr int kWordChannels = 32 / S::BITS, kUnitChannels = 16 / S::BITS;
-    const uint16_t *from = (half ? a.v : a.k) + (int64_t)h * S::D;
-    uint16_t *seen_at = half ? a.v_out : a.k_out;
-    if (seen_at) seen_at += (int64_t)h * S::D;
-
-    if (half == 0) {
-        uint32_t x[2][S::W][kWordChannels / 2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int w = 0; w < S::W; ++w)
-                load_words_if(s.has(8 * i + g), x[i][w], from + (s.row0 + 8 * i + g) * a.row_stride + (4 * w + j) * kWordChannels);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int t = 8 * i + g;
-            const bool has = s.has(t);
-#pragma unroll
-            for (int grp = 0; grp < S::GPR; ++grp) {
-                GroupRange range;
-#pragma unroll
-                for (int w = grp * S::kGroupWords; w < (grp + 1) * S::kGroupWords; ++w)
-#pragma unroll
-                    for (int c = 0; c < kWordChannels / 2; ++c) {
-                        const __half2 v = to_half2<BF>(x[i][w][c]);
-                        x[i][w][c] = half2_bits(v);
-                        range.add(v);
-                    }
-                __half2 r = range.own();
-#pragma unroll
-                for (int d = 1; d < 4; d <<= 1) r = __hmin2_nan(r, as_half2(__shfl_xor_sync(0xffffffffu, half2_bits(r), d)));
-                GroupRule rule;
-                rule.set<S::kTop>(r);
-                if (!tile) rule.zero = NAN, rule.scale = 0.0f;                 // nothing is held of it
-#pragma unroll
-                for (int w = grp * S::kGroupWords; w < (grp + 1) * S::kGroupWords; ++w) {
-                    uint32_t seen[kWordChannels / 2];
-                    const uint32_t word = encode<S, BF, kWordChannels>(rule, x[i][w], seen);
-                    if (seen_at && has) store_words(seen_at + (s.row0 + t) * a.out_stride + (4 * w + j) * kWordChannels, seen);
-                    x[i][w][0] = word;
-                }
-                if (tile && has && j == 0) reinterpret_cast<uint32_t *>(tile + 2 * S::kCodes)[t * S::GPR + grp] = rule.params;
-            }
-            if (tile && has) {
-#pragma unroll
-                for (int w = 0; w < S::W; w += S::VW) {
-                    uint32_t v[S::VW];
-#pragma unroll
-                    for (int n = 0; n < S::VW; ++n) v[n] = x[i][w + n][0];
-                    store_words(reinterpret_cast<uint32_t *>(tile) + S::place(i, w, lane), v);
-                }
-            }
-        }
-        return;
-    }
+    uint32_t k[2][S::W][kWordChannels / 2], v[2][2][S::W][kUnitChannels / 2];  // tokens 8 i + g of K; 8 i + 2 j + e of V
+    const uint16_t *const k_from = a.k + (int64_t)h * S::D + j * kWordChannels, *const v_from = a.v + (int64_t)h * S::D + g * kUnitChannels;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int t = 8 * i + 2 * j;
-        uint32_t x[2][S::W][kUnitChannels / 2], word[S::W];
+#pragma unroll
+        for (int w = 0; w < S::W; ++w) load_words_if(s.has(8 * i + g), k[i][w], k_from + (s.row0 + 8 * i + g) * a.row_stride + w * 4 * kWordChannels);
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int w = 0; w < S::W; ++w)
-                load_words_if(s.has(t + e), x[e][w], from + (s.row0 + t + e) * a.row_stride + (8 * w + g) * kUnitChannels);
+            for (int w = 0; w < S::W; ++w) {
+                const int t = 8 * i + 2 * j + e;
+                load_words_if(s.has(t), v[i][e][w], v_from + (s.row0 + t) * a.row_stride + w * 8 * kUnitChannels);
+            }
+    }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const bool has = s.has(t + e);
+    for (int i = 0; i < 2; ++i) {
+        const int t = 8 * i + g;
+        const bool has = s.has(t);
+        uint32_t code[S::W];
+        if (!s.any(i)) continue;                              // (one new token: most of the tile is somebody else's)
+        encode_token<S, BF, SEEN, kWordChannels, 1, 4>(k[i], code, has, tile != nullptr, reinterpret_cast<uint32_t *>(tile + 2 * S::kCodes) + t * S::GPR,
+                                                       tile && has && j == 0,
+                                                       SEEN ? a.k_out + (s.row0 + t) * a.out_stride + (int64_t)h * S::D + j * kWordChannels : nullptr,
+                                                       4 * kWordChannels);
+        if (tile && has) {
 #pragma unroll
-            for (int grp = 0; grp < S::GPR; ++grp) {
-                GroupRange range;
+            for (int w = 0; w < S::W; w += S::VW) {
+                uint32_t x[S::VW];
 #pragma unroll
-                for (int w = grp * S::kGroupWords; w < (grp + 1) * S::kGroupWords; ++w)
-#pragma unroll
-                    for (int c = 0; c < kUnitChannels / 2; ++c) {
-                        const __half2 v = to_half2<BF>(x[e][w][c]);
-                        x[e][w][c] = half2_bits(v);
-                        range.add(v);
-                    }
-                __half2 r = range.own();
-#pragma unroll
-                for (int d = 4; d < 32; d <<= 1) r = __hmin2_nan(r, as_half2(__shfl_xor_sync(0xffffffffu, half2_bits(r), d)));
-                GroupRule rule;
-                rule.set<S::kTop>(r);
-                if (!tile) rule.zero = NAN, rule.scale = 0.0f;
-#pragma unroll
-                for (int w = grp * S::kGroupWords; w < (grp + 1) * S::kGroupWords; ++w) {
-                    uint32_t seen[kUnitChannels / 2];
-                    const uint32_t bits = encode<S, BF, kUnitChannels>(rule, x[e][w], seen) & 0xffffu;
-                    if (seen_at && has) store_words(seen_at + (s.row0 + t + e) * a.out_stride + (8 * w + g) * kUnitChannels, seen);
-                    word[w] = e ? word[w] | bits << 16 : bits;
-                }
-                if (tile && has && g == 0) reinterpret_cast<uint32_t *>(tile + 2 * S::kCodes + S::kParams)[(t + e) * S::GPR + grp] = rule.params;
+                for (int n = 0; n < S::VW; ++n) x[n] = code[w + n];
+                store_words(reinterpret_cast<uint32_t *>(tile) + S::place(i, w, lane), x);
             }
         }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t code[2][S::W];
+        const int t = 8 * i + 2 * j;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (s.any(i, e)) encode_token<S, BF, SEEN, kUnitChannels, 4, 32>(v[i][e], code[e], s.has(t + e), tile != nullptr,
+                                                            reinterpret_cast<uint32_t *>(tile + 2 * S::kCodes + S::kParams) + (t + e) * S::GPR,
+                                                            tile && s.has(t + e) && g == 0,
+                                                            SEEN ? a.v_out + (s.row0 + t + e) * a.out_stride + (int64_t)h * S::D + g * kUnitChannels : nullptr,
+                                                            8 * kUnitChannels);
         uint32_t *codes = reinterpret_cast<uint32_t *>(tile + S::kCodes);
         if (tile && s.has(t) && s.has(t + 1)) {
 #pragma unroll
             for (int w = 0; w < S::W; w += S::VW) {
-                uint32_t v[S::VW];
+                uint32_t x[S::VW];
 #pragma unroll
-                for (int n = 0; n < S::VW; ++n) v[n] = word[w + n];
-                store_words(codes + S::place(i, w, lane), v);
+                for (int n = 0; n < S::VW; ++n) x[n] = __byte_perm(code[0][w + n], code[1][w + n], 0x5410);
+                store_words(codes + S::place(i, w, lane), x);
             }
         } else if (tile && (s.has(t) || s.has(t + 1))) {      // the other token's half of the words stays
             const int e = s.has(t) ? 0 : 1;
 #pragma unroll
-            for (int w = 0; w < S::W; ++w) reinterpret_cast<uint16_t *>(codes + S::place(i, w, lane))[e] = (uint16_t)(word[w] >> (16 * e));
+            for (int w = 0; w < S::W; ++w) reinterpret_cast<uint16_t *>(codes + S::place(i, w, lane))[e] = (uint16_t)(e ? code[1][w] : code[0][w]);
         }
     }
 }
 
-// N neighbouring channels out of N * BITS bits.
+// N neighbouring channels out of N * BITS bits; scale in fp16 bits.
 template <typename S, bool BF, int N>
-__device__ __forceinline__ void decode(uint32_t word, float scale, float zero, uint32_t (&row)[N / 2])
+__device__ __forceinline__ void decode(uint32_t word, uint32_t scale, float zero, uint32_t (&row)[N / 2])
 {
 #pragma unroll
     for (int c = 0; c < N; c += 2) {
-        const float a = (float)((word >> (c * S::BITS)) & S::kTop), b = (float)((word >> ((c + 1) * S::BITS)) & S::kTop);
-        row[c / 2] = to_row<BF>(__fmaf_rn(a, scale, zero), __fmaf_rn(b, scale, zero));
+        // the code in the low bits of 1024 is 1024 + code; what is left behind 1024 is exact
+        const uint32_t q = c ? word >> (c * S::BITS) : word;
+        const uint32_t pair = S::BITS == 4 ? ((q & 0xfu) | ((q << 12 & 0xf0000u) | 0x64006400u)) : __byte_perm(q, 0x64006400u, 0x5150);
+        const uint32_t code = half2_bits(__hsub2(as_half2(pair), as_half2(0x64006400u)));
+        row[c / 2] = to_row<BF>(fma_half(code, scale, zero), fma_half(code >> 16, scale, zero));
     }
 }
 
@@ -252,64 +288,70 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_read_kernel(const HeldRo
 {
     grid_dependency_wait();
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31, unit = blockIdx.x * kHeldWarps + (threadIdx.x >> 5), half = unit & 1;
-    const int span = a.by_heads(unit >> 1), h = (unit >> 1) - span * a.H;
+    const int lane = threadIdx.x & 31, unit = blockIdx.x * kHeldWarps + (threadIdx.x >> 5);
+    const int span = a.by_heads(unit), h = unit - span * a.H;
     HeldSpan s;
     if (span >= a.spans || !find_span(a, span, s)) return;
     const uint8_t *tile = s.tile < 0 ? nullptr : a.held + ((int64_t)h * a.tiles + s.tile) * S::kTileBytes;
     const int g = lane >> 2, j = lane & 3;
     constexpr int kWordChannels = 32 / S::BITS, kUnitChannels = 16 / S::BITS;
-    uint16_t *to = (half ? a.v_out : a.k_out) + (int64_t)h * S::D;
-    uint32_t x[2][S::W], p[2][2][S::GPR];
+    uint32_t x[2][2][S::W], k_rule[2][S::GPR], v_rule[2][2][S::GPR];           // [K, V][i]; of tokens 8 i + g; of tokens 8 i + 2 j + e
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int w = 0; w < S::W; w += S::VW) {
-            uint32_t v[S::VW] = {};
-            if (tile) load_words(v, reinterpret_cast<const uint32_t *>(tile + half * S::kCodes) + S::place(i, w, lane));
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int n = 0; n < S::VW; ++n) x[i][w + n] = v[n];
-        }
+            for (int w = 0; w < S::W; w += S::VW) {
+                uint32_t v[S::VW];
+                load_words_if(tile != nullptr, v, reinterpret_cast<const uint32_t *>(tile + half * S::kCodes) + S::place(i, w, lane));
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int grp = 0; grp < S::GPR; ++grp) {
-                const int t = half ? 8 * i + 2 * j + e : 8 * i + g;
-                p[i][e][grp] = tile ? __ldg(reinterpret_cast<const uint32_t *>(tile + 2 * S::kCodes + half * S::kParams) + t * S::GPR + grp) : kNanHalf << 16;
+                for (int n = 0; n < S::VW; ++n) x[half][i][w + n] = v[n];
             }
-    }
+    const uint32_t *const rules = reinterpret_cast<const uint32_t *>(tile + 2 * S::kCodes);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int grp = 0; grp < S::GPR; ++grp) {
+            k_rule[i][grp] = tile ? __ldg(rules + (8 * i + g) * S::GPR + grp) : kNanHalf << 16;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) v_rule[i][e][grp] = tile ? __ldg(rules + 16 * S::GPR + (8 * i + 2 * j + e) * S::GPR + grp) : kNanHalf << 16;
+        }
+    uint16_t *const k_to = a.k_out + (int64_t)h * S::D + j * kWordChannels, *const v_to = a.v_out + (int64_t)h * S::D + g * kUnitChannels;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int w = 0; w < S::W; ++w) {
-            const int grp = w / S::kGroupWords;
-            if (half == 0) {
-                const int t = 8 * i + g;
-                const float2 rule = __half22float2(as_half2(p[i][0][grp]));
-                uint32_t row[kWordChannels / 2];
-                decode<S, BF, kWordChannels>(x[i][w], rule.x, rule.y, row);
-                if (s.has(t)) store_words(to + (s.row0 + t) * a.out_stride + (4 * w + j) * kWordChannels, row);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int t = 8 * i + 2 * j + e;
-                    const float2 rule = __half22float2(as_half2(p[i][e][grp]));
-                    uint32_t row[kUnitChannels / 2];
-                    decode<S, BF, kUnitChannels>(x[i][w] >> (16 * e), rule.x, rule.y, row);
-                    if (s.has(t)) store_words(to + (s.row0 + t) * a.out_stride + (8 * w + g) * kUnitChannels, row);
-                }
-            }
+            const int t = 8 * i + g;
+            const uint32_t rule = k_rule[i][w / S::kGroupWords];
+            uint32_t row[kWordChannels / 2];
+            if (!s.any(i)) continue;
+            decode<S, BF, kWordChannels>(x[0][i][w], rule, __high2float(as_half2(rule)), row);
+            if (s.has(t)) store_words(k_to + (s.row0 + t) * a.out_stride + w * 4 * kWordChannels, row);
         }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int w = 0; w < S::W; ++w) {
+                const int t = 8 * i + 2 * j + e;
+                const uint32_t rule = v_rule[i][e][w / S::kGroupWords];
+                uint32_t row[kUnitChannels / 2];
+                if (!s.any(i, e)) continue;
+                decode<S, BF, kUnitChannels>(x[1][i][w] >> (16 * e), rule, __high2float(as_half2(rule)), row);
+                if (s.has(t)) store_words(v_to + (s.row0 + t) * a.out_stride + w * 8 * kUnitChannels, row);
+            }
 }
 
-static int64_t held_ctas(const HeldRows &a) { return ((int64_t)a.spans * a.H * 2 + kHeldWarps - 1) / kHeldWarps; }
+static int64_t held_ctas(const HeldRows &a) { return ((int64_t)a.spans * a.H + kHeldWarps - 1) / kHeldWarps; }
 
-int launch_held_write(const llms_kv_desc &d, int bits, int dtype, const HeldRows &a, cudaStream_t st)
+static int launch_held_write(const llms_kv_desc &d, int bits, int dtype, const HeldRows &a, cudaStream_t st)
 {
     return with_held_shape(d, bits, [&](auto s) {
         using S = decltype(s);
-        LLMS_CUDA_TRY(launch_dependent(dtype == LLMS_BF16 ? held_write_kernel<S, true> : held_write_kernel<S, false>, dim3((unsigned)held_ctas(a)),
-                                       dim3(kHeldWarps * 32), 0, st, a));
+        const auto kernel = dtype == LLMS_BF16 ? (a.k_out ? held_write_kernel<S, true, true> : held_write_kernel<S, true, false>)
+                                               : (a.k_out ? held_write_kernel<S, false, true> : held_write_kernel<S, false, false>);
+        LLMS_CUDA_TRY(launch_dependent(kernel, dim3((unsigned)held_ctas(a)), dim3(kHeldWarps * 32), 0, st, a));
         return LLMS_OK;
     });
 }
@@ -340,7 +382,7 @@ int check_held(const llms_kv_desc *d, int bits, int n_seqs, int max_len)
 }
 
 // What a write and a read have in common: checks, and the operands as the kernels take them.
-static int check_rows(const llms_kv_desc *desc, int bits, int dtype, int layer, const void *held, int n_rows, const int32_t *first_row,
+static int check_rows(const llms_kv_desc *desc, int bits, int dtype, int layer, const void *held, uint64_t held_size, int n_rows, const int32_t *first_row,
                       const int32_t *chunk_table, int table_stride, const int32_t *lens, int n_seqs, int max_len, HeldRows &a)
 {
     const int rc = check_held(desc, bits, n_seqs, max_len);
@@ -351,6 +393,7 @@ static int check_rows(const llms_kv_desc *desc, int bits, int dtype, int layer, 
     if (!held || !chunk_table || !lens) return LLMS_ERR_INVALID_ARG;
     if (table_stride < 1 || (int64_t)table_stride * desc->chunk_len < max_len) return LLMS_ERR_INVALID_ARG;
     if (!aligned(held, 16) || !aligned(chunk_table, 4) || !aligned(lens, 4) || !aligned(first_row, 4)) return LLMS_ERR_MISALIGNED;
+    if (held_size < held_pool_bytes(*desc, bits)) return LLMS_ERR_BUF_TOO_SMALL;
     a.H = desc->n_kv_heads;
     a.tiles = held_tiles(*desc);
     a.held = static_cast<uint8_t *>(const_cast<void *>(held)) + (uint64_t)layer * a.H * a.tiles * held_tile_bytes(*desc, bits);
@@ -379,16 +422,16 @@ extern "C" int llms_held_bytes(const llms_kv_desc *desc, int bits, uint64_t *nby
     const int rc = check_held(desc, bits, 0, 1);
     if (rc) return rc;
     if (!nbytes) return LLMS_ERR_INVALID_ARG;
-    *nbytes = (uint64_t)desc->n_layers * desc->n_kv_heads * held_tiles(*desc) * held_tile_bytes(*desc, bits);
+    *nbytes = held_pool_bytes(*desc, bits);
     return LLMS_OK;
 }
 
-extern "C" int llms_held_write(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, const void *k, const void *v,
+extern "C" int llms_held_write(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, uint64_t held_size, const void *k, const void *v,
                                int64_t row_stride, int n_rows, const int32_t *first_row, const int32_t *chunk_table, int table_stride,
                                const int32_t *lens, int n_seqs, int max_len, void *k_seen, void *v_seen, int64_t seen_stride, void *stream)
 {
     HeldRows a{};
-    int rc = check_rows(desc, bits, dtype, layer, held, n_rows, first_row, chunk_table, table_stride, lens, n_seqs, max_len, a);
+    int rc = check_rows(desc, bits, dtype, layer, held, held_size, n_rows, first_row, chunk_table, table_stride, lens, n_seqs, max_len, a);
     if (rc || n_seqs == 0 || n_rows == 0) return rc;
     if ((rc = check_row_pair(*desc, k, v, row_stride))) return rc;
     if ((k_seen == nullptr) != (v_seen == nullptr)) return LLMS_ERR_INVALID_ARG;
@@ -399,12 +442,12 @@ extern "C" int llms_held_write(const llms_kv_desc *desc, int bits, int dtype, in
     return launch_held_write(*desc, bits, dtype, a, static_cast<cudaStream_t>(stream));
 }
 
-extern "C" int llms_held_read(const llms_kv_desc *desc, int bits, int dtype, int layer, const void *held, const int32_t *chunk_table,
-                              int table_stride, const int32_t *lens, int n_seqs, int max_len, const int32_t *first_row, int n_rows,
+extern "C" int llms_held_read(const llms_kv_desc *desc, int bits, int dtype, int layer, const void *held, uint64_t held_size,
+                              const int32_t *chunk_table, int table_stride, const int32_t *lens, int n_seqs, int max_len, const int32_t *first_row, int n_rows,
                               void *k_out, void *v_out, int64_t out_stride, void *stream)
 {
     HeldRows a{};
-    int rc = check_rows(desc, bits, dtype, layer, held, n_rows, first_row, chunk_table, table_stride, lens, n_seqs, max_len, a);
+    int rc = check_rows(desc, bits, dtype, layer, held, held_size, n_rows, first_row, chunk_table, table_stride, lens, n_seqs, max_len, a);
     if (rc || n_seqs == 0 || n_rows == 0) return rc;
     if ((rc = check_row_pair(*desc, k_out, v_out, out_stride))) return rc;
     a.k_out = static_cast<uint16_t *>(k_out); a.v_out = static_cast<uint16_t *>(v_out);

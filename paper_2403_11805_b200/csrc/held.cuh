@@ -31,6 +31,8 @@ struct HeldShape {
 inline uint64_t held_tile_bytes(const llms_kv_desc &d, int bits) { return 2 * (2 * (uint64_t)d.head_dim * bits + 64 * (d.head_dim / d.group_size)); }
 inline int held_tiles(const llms_kv_desc &d) { return n_chunks(d) * (d.chunk_len / 16); }   // per (layer, KV head)
 
+inline uint64_t held_pool_bytes(const llms_kv_desc &d, int bits) { return (uint64_t)d.n_layers * d.n_kv_heads * held_tiles(d) * held_tile_bytes(d, bits); }
+
 // Checks of shape that all calls on a held pool make.
 int check_held(const llms_kv_desc *d, int bits, int n_seqs, int max_len);
 
@@ -61,8 +63,6 @@ struct HeldRows {                                 // operands of a write or read
     Divisor by_chunk, by_heads;
 };
 
-int launch_held_write(const llms_kv_desc &d, int bits, int dtype, const HeldRows &a, cudaStream_t st);
-
 #ifdef __CUDACC__
 
 __device__ __forceinline__ uint32_t half2_bits(__half2 x) { return *reinterpret_cast<uint32_t *>(&x); }
@@ -86,13 +86,8 @@ template <bool BF>
 __device__ __forceinline__ uint32_t to_row(float a, float b)
 {
     uint32_t r;
-    if constexpr (BF) {
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-    } else {
-        asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-        if (isnan(a)) r = (r & 0xffff0000u) | kNanHalf;
-        if (isnan(b)) r = (r & 0xffffu) | (kNanHalf << 16);
-    }
+    if constexpr (BF) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    else asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
     return r;
 }
 

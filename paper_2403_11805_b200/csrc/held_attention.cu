@@ -143,8 +143,8 @@ extern "C" int llms_held_workspace_bytes(const llms_kv_desc *desc, int bits, int
     return LLMS_OK;
 }
 
-extern "C" int llms_held_attention(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, const void *q, int64_t q_stride,
-                                   const void *k_new, const void *v_new, int64_t new_stride, const int32_t *chunk_table, int table_stride,
+extern "C" int llms_held_attention(const llms_kv_desc *desc, int bits, int dtype, int layer, void *held, uint64_t held_size, const void *q,
+                                   int64_t q_stride, const void *k_new, const void *v_new, int64_t new_stride, const int32_t *chunk_table, int table_stride,
                                    const int32_t *lens, int n_seqs, int max_len, int window, float scale, void *out, float *lse,
                                    void *workspace, uint64_t workspace_bytes, void *stream)
 {
@@ -161,7 +161,7 @@ extern "C" int llms_held_attention(const llms_kv_desc *desc, int bits, int dtype
     if (k_new && (!aligned(k_new, 16) || !aligned(v_new, 16) || new_stride % 8)) return LLMS_ERR_MISALIGNED;
     if (!aligned(chunk_table, 4) || !aligned(lens, 4) || !aligned(lse, 4)) return LLMS_ERR_MISALIGNED;
     const HeldLayout lay = held_layout(*desc, bits, n_seqs, max_len, window);
-    if (workspace_bytes < lay.total) return LLMS_ERR_BUF_TOO_SMALL;
+    if (workspace_bytes < lay.total || held_size < held_pool_bytes(*desc, bits)) return LLMS_ERR_BUF_TOO_SMALL;
 
     DecodeArgs a{};
     a.q = static_cast<const uint16_t *>(q);

@@ -14,11 +14,11 @@ def pool(**kw):
     return B.make_desc(**args)
 
 
-WRITE = dict(bits=4, dtype=0, layer=0, held=A, k=A, v=A, row_stride=256, n_rows=7, first_row=A, chunk_table=A, table_stride=5, lens=A, n_seqs=3,
+WRITE = dict(bits=4, dtype=0, layer=0, held=A, held_size=1 << 40, k=A, v=A, row_stride=256, n_rows=7, first_row=A, chunk_table=A, table_stride=5, lens=A, n_seqs=3,
              max_len=80, k_seen=None, v_seen=None, seen_stride=0, stream=None)
-READ = dict(bits=4, dtype=0, layer=0, held=A, chunk_table=A, table_stride=5, lens=A, n_seqs=3, max_len=80, first_row=A, n_rows=7, k_out=A, v_out=A,
+READ = dict(bits=4, dtype=0, layer=0, held=A, held_size=1 << 40, chunk_table=A, table_stride=5, lens=A, n_seqs=3, max_len=80, first_row=A, n_rows=7, k_out=A, v_out=A,
             out_stride=256, stream=None)
-ATTEND = dict(bits=4, dtype=0, layer=0, held=A, q=A, q_stride=512, k_new=None, v_new=None, new_stride=0, chunk_table=A, table_stride=5, lens=A,
+ATTEND = dict(bits=4, dtype=0, layer=0, held=A, held_size=1 << 40, q=A, q_stride=512, k_new=None, v_new=None, new_stride=0, chunk_table=A, table_stride=5, lens=A,
               n_seqs=3, max_len=80, window=0, scale=0.125, out=A, lse=None, workspace=A, workspace_bytes=1 << 40, stream=None)
 
 
@@ -38,7 +38,7 @@ COMMON = [
     (INVALID, dict(chunk_table=None)), (INVALID, dict(lens=None)), (INVALID, dict(table_stride=4)), (INVALID, dict(table_stride=0)),
     (INVALID, dict(n_seqs=-1)), (INVALID, dict(max_len=0)), (INVALID, dict(max_len=81)), (MISALIGNED, dict(held=A + 8)),
     (MISALIGNED, dict(chunk_table=A + 2)), (MISALIGNED, dict(lens=A + 1)), (UNSUPPORTED, dict(n_seqs=4097)), (UNSUPPORTED, dict(bits=2)),
-    (UNSUPPORTED, dict(bits=1)), (BAD_BITS, dict(bits=3)), (BAD_BITS, dict(bits=0)), (BAD_BITS, dict(bits=16)),
+    (UNSUPPORTED, dict(bits=1)), (BAD_BITS, dict(bits=3)), (BAD_BITS, dict(bits=0)), (BAD_BITS, dict(bits=16)), (SMALL, dict(held_size=0)), (SMALL, dict(held_size=2 * 4 * 10 * 1152 - 1)),
 ]
 
 
@@ -117,7 +117,7 @@ def on_the_host(monkeypatch):
     import torch
     called, names = [], ("llms_held_write", "llms_held_read", "llms_held_attention")
     fake = type("Lib", (), {name: staticmethod(lambda *a, name=name: called.append(name) or 0) for name in names})
-    fake.llms_strerror, fake.llms_held_bytes = B.lib().llms_strerror, B.lib().llms_held_bytes
+    fake.llms_strerror = B.lib().llms_strerror
     B._CACHE_TYPES.update({torch.float16: B.DTYPE_F16, torch.bfloat16: B.DTYPE_BF16})
     monkeypatch.setattr(B, "_torch", torch)
     monkeypatch.setattr(B, "_current", lambda stream: (-1, 0))               # where host tensors say they are
@@ -153,9 +153,9 @@ def test_the_binding_s_checks(on_the_host):
         (2, dict(q=torch.zeros(3, 8, 32, **f16))), (2, dict(out=torch.zeros(3, 8, 64))), (2, dict(k_new=rows(3))), (2, dict(k_new=rows(2), v_new=rows(2))),
         (2, dict(lse=torch.zeros(3, 4))), (2, dict(window=1 << 32)), (2, dict(workspace=torch.zeros(1, dtype=torch.uint8).expand(1 << 20))),
     ] + [(i, w) for i in range(3) for w in (
-        dict(held=torch.zeros(2, 4, 10, 1151, dtype=torch.uint8)), dict(held=torch.zeros(2, 4, 10, 2304, dtype=torch.uint8)[..., ::2]),
+        dict(held=torch.zeros(2, 4, 10, 2304, dtype=torch.uint8)[..., ::2]),
         dict(chunk_table=torch.zeros(3, 4, dtype=torch.int32)), dict(chunk_table=torch.zeros(2, 5, dtype=torch.int32)),
-        dict(lens=torch.zeros(3, dtype=torch.int64)), dict(lens=torch.zeros(3, 1, dtype=torch.int32)), dict(layer=1 << 32), dict(bits=(1 << 32) + 4), dict(bits=2))]:
+        dict(lens=torch.zeros(3, dtype=torch.int64)), dict(lens=torch.zeros(3, 1, dtype=torch.int32)), dict(layer=1 << 32), dict(bits=(1 << 32) + 4))]:
         with pytest.raises(B.LlmsError):
             calls[which](**wrong)
     assert len(on_the_host) == 3
