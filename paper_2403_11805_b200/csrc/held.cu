@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_write_kernel(const HeldR
 {
     grid_dependency_wait();
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31, unit = blockIdx.x * kHeldWarps + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, unit = blockIdx.x * kHeldWarps + __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int span = a.by_heads(unit), h = unit - span * a.H;
     HeldSpan s;
     if (span >= a.spans || !find_span(a, span, s)) return;
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_read_kernel(const HeldRo
 {
     grid_dependency_wait();
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31, unit = blockIdx.x * kHeldWarps + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, unit = blockIdx.x * kHeldWarps + __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int span = a.by_heads(unit), h = unit - span * a.H;
     HeldSpan s;
     if (span >= a.spans || !find_span(a, span, s)) return;

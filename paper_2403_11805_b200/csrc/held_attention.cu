@@ -174,6 +174,8 @@ extern "C" int llms_held_attention(const llms_kv_desc *desc, int bits, int dtype
     a.table_stride = table_stride; a.n_seqs = n_seqs; a.max_len = max_len; a.window = window;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     set_decode_shape(a, *desc, lay, ws, scale);
+    // the kernel counts an item's tiles and kItemSlots more in 32 bits
+    if (((uint64_t)max_len / kHeldTile + 1 + kItemSlots) * n_seqs * a.Hkv * a.blocks > 0x7fffffff) return LLMS_ERR_UNSUPPORTED;
     HeldFeed f{};
     f.tiles = held_tiles(*desc);
     f.held = static_cast<uint8_t *>(held) + (uint64_t)layer * a.Hkv * f.tiles * held_tile_bytes(*desc, bits);

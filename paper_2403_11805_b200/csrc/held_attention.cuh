@@ -245,9 +245,9 @@ __device__ __forceinline__ void join_parts(const DecodeArgs &a, bool bf16, const
 }
 
 // How the batch is cut into runs: into equal numbers of slots.  An item has a slot per tile and kItemSlots in front of them for what it costs
-// to begin and end one (query rows, first maxima, the newest token, results: about as much as three tiles), so that a run through
+// to begin and end one (query rows, first maxima, the newest token, results: about as much as five tiles), so that a run through
 // many short items is not the one that all wait for.
-constexpr int kItemSlots = 3;
+constexpr int kItemSlots = 5;
 struct HeldCut {
     int w0, w1;                                   // the run's tiles, in the batch's numbering
     int seq, base, slot;                          // the sequence of the first one, the numbers of its first tile and of its first slot
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
                                                               // query row << 8, 64 or 32: the newest token's row goes into
                                                               // the first, second half, 128: a half lies outside the pool
     __shared__ HeldPlace s_place[W];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, run = ITEM ? blockIdx.x : blockIdx.x * W + warp, g = lane >> 2, j = lane & 3;
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), run = ITEM ? blockIdx.x : blockIdx.x * W + warp, g = lane >> 2, j = lane & 3;
     unsigned char *const ring = smem_held + warp * kStages * f.stage_bytes;
     if constexpr (ITEM) cluster_arrive();                     // this CTA has begun: the others may store into its shared memory
     grid_dependency_wait();
