@@ -11,6 +11,10 @@
 // of the groups.  All its loads are under way before the first value is used.  A sequence's rows may begin and end inside
 // a tile: the other tokens' codes in it are left as they are.  Neighbouring warps take the heads of the same tokens, whose
 // rows lie side by side.
+//
+// Measured, a B200, 4 bits: a prompt of 32768 tokens, 8 heads of 128 channels, written in 34 to 36 us (170 MB, 4.7 to 4.9 TB/s; 11
+// instructions per channel: 60% of the issue slots); 4096 tokens of 32 heads read in 16.2 us (85 MB, 5.2 TB/s); one token for each of
+// 32 sequences, one head of 256 channels at 8 bits, 5.2 us.  K and V in warps of their own: 55 and 22 us.
 #include <algorithm>
 #include <type_traits>
 

@@ -7,12 +7,19 @@
 // 2^-24 (or 2^-20, four bits further up), exactly.  So a mask, for half of the codes a shift too, makes a pair of operands, the products
 // are exact, and the powers of two are taken back in the sums.
 //
-// Bound.  A quarter (half) of the fp16 pool's bytes for the same arithmetic: at 4 bits and 128 channels an SM has some 95 cycles per
-// tile of 2176 bytes at the copy bandwidth, and a tile takes about 200 instructions of a warp.  So both count: the
-// instructions must be few, and enough warps must be there to fill each other's gaps.
+// Bound.  A quarter (half) of the fp16 pool's bytes for the same arithmetic: at 4 bits and 128 channels an SM has some 80 cycles per 16
+// tokens at the copy bandwidth, in which its four schedulers issue at most 320 instructions; 16 tokens take 250, half of
+// them logical ones that hold their pipe for two cycles.  So it is the arithmetic that bounds large batches (without its copies
+// the kernel takes the same time), and the latencies of length, table, tile and join that bound small calls.
 //
-// Split.  As for the fp16 pool: runs of 16-token tiles, one per warp, or a cluster per item for small calls.  A tile is one
-// run of bytes in the pool and comes as one copy; its codes lie in the order of the MMAs' operands.
+// Split.  As for the fp16 pool: runs of tiles, one per warp, or a cluster per item for small calls.  A tile of the pool is one run of bytes,
+// copied by a warp's own lanes (cp.async: a third of the instructions that one lane's bulk copies and their barriers took), and
+// its codes lie in the order of the MMAs' operands, so that they go from shared memory into masks and MMAs.  The
+// parts of a cluster's warps are stored into the shared memory of the CTA that joins them: one barrier, no reads across.
+//
+// Measured, a B200: 16 contexts of 4096 tokens, 32 heads of 128 channels at 4 bits 64 us (286 MB, 4.5 TB/s; 164 us in the fp16 pool); one
+// grouped-query context of 32768 tokens 20.3 us; one context of 4096 tokens 10.9; one of 256 tokens, 4 heads of 64, 4.2.
+// Warps per SM for the batch: 12 72 us, 16 64, 20 66 (96 registers: spills).
 #pragma once
 
 #include "decode.cuh"
@@ -319,7 +326,11 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
     constexpr int kCols = DecodeCols<(S::D + 63) / 64>::kCols, kPitch = DecodeCols<(S::D + 63) / 64>::kPitch;
     constexpr int MT = S::D / 16, GPR = S::GPR;               // 16-channel tiles of the output; groups per row
     constexpr bool k4 = S::BITS == 4;
-    constexpr uint32_t kLow = k4 ? 0x000f000fu : 0x00ff00ffu, kHigh = 0x00f000f0u;
+    // Codes of 4 bits are moved up by two places: an MMA keeps its sums to 24 bits or so below the operands' exponents, and a subnormal
+    // operand's exponent is that of its top place, however few of the ten places it fills (moved up, results come four times nearer)
+    constexpr uint32_t kLow = k4 ? 0x003c003cu : 0x00ff00ffu, kHigh = 0x03c003c0u;
+    constexpr int kUp = k4 ? 2 : 0, kDown = 8 - kUp;
+    constexpr float kUnit = k4 ? 0x1p22f : 0x1p24f, kMiddle = (float)S::kTop / 2;             // (in the high places 16 times the low ones')
     constexpr int W = ITEM ? HeldParts<S>::kWarps : kRunWarps, N = HeldParts<S>::N;
     extern __shared__ __align__(128) unsigned char smem_held[];
     __shared__ int4 s_feed[W][kAhead];                        // tiles looked up: the two tiles of the pool; sequence; query rows, first
@@ -428,10 +439,11 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
 
         // ---- the arithmetic's state
         uint32_t qf[NT][S::W][k4 ? 4 : 2];
-        float o[NT][MT][4], ref[NT][NC], limit[NT][NC], l[NT][NC], zero_sum[NT][GPR][NC], fac[NT][NC], q_sum[NT][GPR][NC];
+        float o[NT][MT][4], ref[NT][NC], limit[NT][NC], l[NT][NC], zero_sum[NT][GPR][NC], w_sum[NT][GPR][NC], fac[NT][NC], q_sum[NT][GPR][NC];
         float lift = 1.0f, scale_limit = -1.0f;               // what V's scales are multiplied with; the largest one that this suits
         int left = 0, odd_first = 0, odd_last = 0;            // tiles of the item in this run; what `left` is at its first and last tile if
                                                               // those may hold places nobody sees or the newest token (else -1)
+        const float middle = kTwin && (lane & 2) ? 0.0f : -kMiddle / kUnit;                // of the columns of whole weights
         const uint32_t cut = lane & 2 ? 0xffffe000u : 0u;     // keeps what fp16 holds of a weight
         bool begins = true, started = false;                  // the item's first tile here is next; the item has had a tile
 
@@ -524,7 +536,7 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
 #pragma unroll
                         for (int i = 0; i < NC; ++i) {
                             q_sum[nt][grp][i] = sums[i];
-                            zero_sum[nt][grp][i] = 0.0f;
+                            zero_sum[nt][grp][i] = w_sum[nt][grp][i] = 0.0f;
                             if (!isfinite(sums[i])) fac[nt][i] = NAN;
                         }
                     }
@@ -597,9 +609,9 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
 #pragma unroll
                         for (int n = 0; n < VW; ++n) {
                             const int w = grp * S::kGroupWords + v + n;
-                            const uint32_t y0 = x0[n] >> 8, y1 = x1[n] >> 8;
-                            const uint32_t low[4] = {x0[n] & kLow, x1[n] & kLow, y0 & kLow, y1 & kLow};
-                            const uint32_t high[4] = {x0[n] & kHigh, x1[n] & kHigh, y0 & kHigh, y1 & kHigh};
+                            const uint32_t z0 = x0[n] << kUp, z1 = x1[n] << kUp, y0 = x0[n] >> kDown, y1 = x1[n] >> kDown;
+                            const uint32_t low[4] = {z0 & kLow, z1 & kLow, y0 & kLow, y1 & kLow};
+                            const uint32_t high[4] = {z0 & kHigh, z1 & kHigh, y0 & kHigh, y1 & kHigh};
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
                                 float (&c)[4] = k4 || (v + n) % 2 == 0 ? c0[nt] : c1[nt];
@@ -613,8 +625,7 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
                         }
                     }
                     const float2 r0 = __half22float2(rule[g * GPR + grp]), r1 = __half22float2(rule[(8 + g) * GPR + grp]);
-                    constexpr float kUnit = k4 ? 0x1p20f : 0x1p24f;
-                    const float m0 = r0.x * kUnit, m1 = r1.x * kUnit;
+                    const float m0 = r0.x * (k4 ? kUnit / 16 : kUnit), m1 = r1.x * (k4 ? kUnit / 16 : kUnit);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -642,7 +653,7 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
                             if (t < place.first || t >= place.len) s[u][nt][i] = -INFINITY;
                         }
             }
-            float2 v_rule[2][GPR][2];                         // V's scales and zero-points of this lane's tokens
+            float2 v_rule[2][GPR][2];                         // V's scales and the values of the middle code, of this lane's tokens
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const __half2 *const rule = reinterpret_cast<const __half2 *>(mem + u * S::kTileBytes + 2 * S::kCodes + S::kParams);
@@ -651,6 +662,7 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         v_rule[u][grp][i] = __half22float2(rule[(8 * i + g) * GPR + grp]);
+                        v_rule[u][grp][i].y = __fmaf_rn(v_rule[u][grp][i].x, kMiddle, v_rule[u][grp][i].y);
                         over |= v_rule[u][grp][i].x > scale_limit;
                     }
 #pragma unroll
@@ -696,7 +708,10 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
                         for (int i = 0; i < NC; ++i) {
                             l[nt][i] *= keep[nt][i];
 #pragma unroll
-                            for (int grp = 0; grp < GPR; ++grp) zero_sum[nt][grp][i] *= keep[nt][i];
+                            for (int grp = 0; grp < GPR; ++grp) {
+                                zero_sum[nt][grp][i] *= keep[nt][i];
+                                w_sum[nt][grp][i] *= keep[nt][i] * change;
+                            }
                         }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -732,6 +747,7 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
                                 const float w = s[u][nt][hh * NC + i];
                                 zero_sum[nt][grp][i] = __fmaf_rn(w, v_rule[u][grp][hh].y, zero_sum[nt][grp][i]);
                                 p[i] = w * m;
+                                w_sum[nt][grp][i] += p[i];
                             }
                             if constexpr (kTwin) {
                                 // the first four columns get the weights cut off to fp16, the others what was cut off
@@ -754,9 +770,9 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
 #pragma unroll
                         for (int n = 0; n < VW; ++n) {
                             const int w = grp * S::kGroupWords + v + n;
-                            const uint32_t y0 = x0[n] >> 8, y1 = x1[n] >> 8;
+                            const uint32_t z0 = x0[n] << kUp, z1 = x1[n] << kUp, y0 = x0[n] >> kDown, y1 = x1[n] >> kDown;
                             if constexpr (k4) {
-                                const uint32_t f0[4] = {x0[n] & kLow, x0[n] & kHigh, x1[n] & kLow, x1[n] & kHigh};
+                                const uint32_t f0[4] = {z0 & kLow, z0 & kHigh, z1 & kLow, z1 & kHigh};
                                 const uint32_t f1[4] = {y0 & kLow, y0 & kHigh, y1 & kLow, y1 & kHigh};
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
@@ -768,7 +784,7 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
                                     }
                                 }
                             } else {
-                                const uint32_t f0[4] = {x0[n] & kLow, y0 & kLow, x1[n] & kLow, y1 & kLow};
+                                const uint32_t f0[4] = {z0 & kLow, y0 & kLow, z1 & kLow, y1 & kLow};
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
                                     mma_add(o[nt][w], f0, p_hi[nt][0], p_hi[nt][1]);
@@ -778,6 +794,28 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
                         }
                     }
                 }
+            }
+            // The sums over codes are held about the middle code: taken as they are they grow with the number of tokens while the result does
+            // not, and an MMA cuts its sums off.  Every few tiles, and at the end, the middle is taken out of what has come in (a batch
+            // of 16 contexts of 4096 tokens: 1.01 times the error that the rounding of the output has, at the end only 1.03; no time)
+            if (left == 1 || (left & 3) == 0) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int grp = 0; grp < GPR; ++grp) {
+                        float low[NC];
+#pragma unroll
+                        for (int i = 0; i < NC; ++i) {
+#pragma unroll
+                            for (int d = 4; d < 32; d <<= 1) w_sum[nt][grp][i] += __shfl_xor_sync(0xffffffffu, w_sum[nt][grp][i], d);
+                            low[i] = w_sum[nt][grp][i] * middle;
+                            w_sum[nt][grp][i] = 0.0f;
+                        }
+#pragma unroll
+                        for (int t = grp * (MT / GPR); t < (grp + 1) * (MT / GPR); ++t)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[nt][t][i] = __fmaf_rn(low[i % NC], k4 && i >= 2 ? 16.0f : 1.0f, o[nt][t][i]);
+                    }
             }
             __syncwarp();                                     // the stage may be filled again
             poisoned >>= 1;
@@ -805,7 +843,7 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[0][t][i] += __shfl_xor_sync(0xffffffffu, o[0][t][i], 2);
             }
-            const float unit0 = kLift * 0x1p24f * __uint_as_float((254u << 23) - __float_as_uint(lift)), unit1 = k4 ? unit0 * 0x1p-4f : unit0;
+            const float unit0 = kLift * kUnit * __uint_as_float((254u << 23) - __float_as_uint(lift)), unit1 = k4 ? unit0 * 0x1p-4f : unit0;
             // where a partial result goes: a place of the workspace, or the places of the cluster's CTAs
             float *part = a.part + ((int64_t)run * 2 + (began ? 1 : 0)) * a.rows * kPitch;
             const float *const parts = reinterpret_cast<const float *>(smem_held + W * kStages * f.stage_bytes);
