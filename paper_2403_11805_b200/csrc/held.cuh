@@ -67,7 +67,7 @@ struct HeldRows {                                 // operands of a write or read
 
 __device__ __forceinline__ uint32_t half2_bits(__half2 x) { return *reinterpret_cast<uint32_t *>(&x); }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<__half2 *>(&x); }
-constexpr uint32_t kNanHalf = 0x7e00u, kNanBfloat = 0x7fc0u;
+constexpr uint32_t kNanHalf = 0x7e00u;
 
 // A pair of a row's values as fp16: bfloat16 to nearest, saturated, its infinities and NaN as NaN.
 template <bool BF>

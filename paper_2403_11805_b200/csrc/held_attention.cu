@@ -47,14 +47,18 @@ __global__ void __launch_bounds__(kFinishThreads) held_finish_kernel(const Decod
 {
     __shared__ float4 s_acc[kFinishThreads];
     __shared__ float2 s_ml[kFinishThreads / 16];
+    const int x = by_rows(blockIdx.x), r = blockIdx.x - x * a.rows, per_seq = a.Hkv * a.blocks;
+    // (the lengths are older than the kernel before, which has begun: they need not be waited for.  No CTA ends before the wait: the
+    // kernel behind this one waits for this one only)
+    const bool empty = by_item && seq_tiles<kHeldTile>(a, __ldg(a.lens + a.by_per_seq(x))).n == 0;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int x = by_rows(blockIdx.x), r = blockIdx.x - x * a.rows, item = by_item ? x : __ldcg(a.open + x);
-    if (item < 0) return;
+    const int item = by_item ? x : __ldcg(a.open + x);
+    if (empty || item < 0) return;
     const int2 span = __ldcg(a.span + item);
-    const int per_seq = a.Hkv * a.blocks, b = a.by_per_seq(item), hb = item - b * per_seq, h = a.by_blocks(hb), rb = hb - h * a.blocks;
+    const int b = a.by_per_seq(item), hb = item - b * per_seq, h = a.by_blocks(hb), rb = hb - h * a.blocks;
     const int row = rb * (a.group > 8 ? 16 : 8) + r;          // of the KV head's
-    if (row >= a.group || (by_item && seq_tiles<kHeldTile>(a, __ldg(a.lens + b)).n == 0) || span.x < 0) return;
+    if (row >= a.group || span.x < 0) return;
     const int groups = cols / 4, slices = kFinishThreads / groups, slice = threadIdx.x / groups, c = (threadIdx.x - slice * groups) * 4, pitch = cols + 4;
     const float *const from = a.part + (int64_t)r * pitch;
     const int64_t stride = (int64_t)a.rows * pitch;
