@@ -346,8 +346,9 @@ int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float *mass, int
 /* ------------------------------------------------------------------ a cache held at 8 or 4 bits */
 
 /* A second kind of pool, for contexts that stay resident at few bits: K and V are quantised token by token as they are written,
- * by the rule of the swap records (a group is group_size channels of one token of one KV head; see the record format above),
- * and attention reads the codes.  `desc` gives the pool's shape as above (n_tokens = slots * chunk_len; quant_mode 0; the strides are
+ * by the rule of the swap records (a group is group_size channels of one token of one KV head; see the record format above; the
+ * scale is (max x - min x) times the binary32 number next to 1 / (2^b - 1), so that where the quotient lies half-way between two
+ * fp16 numbers it may be the other one), and attention reads the codes.  `desc` gives the pool's shape as above (n_tokens = slots * chunk_len; quant_mode 0; the strides are
  * checked but have no influence) and `bits` (4 or 8) the width of its codes.  A held pool is llms_held_bytes(desc, bits) bytes,
  *     [n_layers][n_kv_heads][tile][K codes | V codes | K parameters | V parameters],
  * a tile being 16 consecutive rows of the pool.  Parameters: [token][group] of {u16 scale, u16 zero-point} (fp16 bits).  With

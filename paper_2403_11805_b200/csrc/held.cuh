@@ -107,7 +107,7 @@ struct GroupRange {
 };
 
 // Scale and zero-point of a group and what its codes are made with; the rule is the swap records' (binary32, to nearest, nothing
-// fused).
+// fused), but for the scale, which is a product with 1 / (2^b - 1) instead of a quotient.
 struct GroupRule {
     float zero, inverse, scale;                   // a group with an infinity or a NaN: zero is NaN, all codes are 0
     uint32_t params;                              // (scale, zero) in fp16
@@ -116,7 +116,7 @@ struct GroupRule {
     {
         const float low = __half2float(__low2half(range)), high = -__half2float(__high2half(range));
         const bool finite = isfinite(low) && isfinite(high);
-        const __half s = finite ? __float2half_rn(__fdiv_rn(fabsf(__fsub_rn(high, low)), (float)TOP)) : __ushort_as_half(0);
+        const __half s = finite ? __float2half_rn(__fmul_rn(fabsf(__fsub_rn(high, low)), 1.0f / TOP)) : __ushort_as_half(0);
         zero = finite ? __fadd_rn(low, 0.0f) : NAN;
         scale = __half2float(s);
         inverse = scale == 0.0f ? 0.0f : __frcp_rn(scale);

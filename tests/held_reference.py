@@ -24,7 +24,7 @@ def quantise(x, bits, span):
         bad = ~np.isfinite(g).all(-1)
         low, high = g.min(-1) + np.float32(0), g.max(-1)
         top = np.float32(2 ** bits - 1)
-        scale = (np.abs(high - low) / top).astype(np.float16)      # (a range of 0 is +0 whatever the zeros' signs)
+        scale = (np.abs(high - low) * (np.float32(1) / top)).astype(np.float16)      # (a range of 0 is +0 whatever the zeros' signs)
         s32 = scale.astype(np.float32)
         inverse = np.float32(1) / s32
         codes = np.minimum(np.rint((g - low[..., None]) * inverse[..., None]), top)
