@@ -80,18 +80,15 @@ template <> struct Words<1> { using T = uint32_t; };
 template <> struct Words<2> { using T = uint2; };
 template <> struct Words<4> { using T = uint4; };
 
-// N words from or to an address that is aligned to them.
-template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&x)[N], const void *p)
-{
-    using T = typename Words<N>::T;
-    *reinterpret_cast<T *>(x) = __ldg(reinterpret_cast<const T *>(p));
-}
-template <int N>
+// N words from or to an address that is aligned to them.  WRITTEN: the kernel stores to that memory too (rows whose held values
+// take their place), so that the load must not be one of memory that stays as it is.
+template <bool WRITTEN, int N>
 __device__ __forceinline__ void load_words_if(bool there, uint32_t (&x)[N], const void *p)
 {
+    using T = typename Words<N>::T;
     if (there) {
-        load_words(x, p);
+        if constexpr (WRITTEN) *reinterpret_cast<T *>(x) = *reinterpret_cast<const T *>(p);
+        else *reinterpret_cast<T *>(x) = __ldg(reinterpret_cast<const T *>(p));
     } else {
 #pragma unroll
         for (int c = 0; c < N; ++c) x[c] = 0u;
@@ -216,13 +213,13 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_write_kernel(const HeldR
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int w = 0; w < S::W; ++w) load_words_if(s.has(8 * i + g), k[i][w], k_from + (s.row0 + 8 * i + g) * a.row_stride + w * 4 * kWordChannels);
+        for (int w = 0; w < S::W; ++w) load_words_if<SEEN>(s.has(8 * i + g), k[i][w], k_from + (s.row0 + 8 * i + g) * a.row_stride + w * 4 * kWordChannels);
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int w = 0; w < S::W; ++w) {
                 const int t = 8 * i + 2 * j + e;
-                load_words_if(s.has(t), v[i][e][w], v_from + (s.row0 + t) * a.row_stride + w * 8 * kUnitChannels);
+                load_words_if<SEEN>(s.has(t), v[i][e][w], v_from + (s.row0 + t) * a.row_stride + w * 8 * kUnitChannels);
             }
     }
 #pragma unroll
@@ -307,7 +304,7 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_read_kernel(const HeldRo
 #pragma unroll
             for (int w = 0; w < S::W; w += S::VW) {
                 uint32_t v[S::VW];
-                load_words_if(tile != nullptr, v, reinterpret_cast<const uint32_t *>(tile + half * S::kCodes) + S::place(i, w, lane));
+                load_words_if<false>(tile != nullptr, v, reinterpret_cast<const uint32_t *>(tile + half * S::kCodes) + S::place(i, w, lane));
 #pragma unroll
                 for (int n = 0; n < S::VW; ++n) x[half][i][w + n] = v[n];
             }
