@@ -346,9 +346,14 @@ int llms_evict_tokens(const llms_kv_desc *desc, void *kv, const float *mass, int
 /* ------------------------------------------------------------------ a cache held at 8 or 4 bits */
 
 /* A second kind of pool, for contexts that stay resident at few bits: K and V are quantised token by token as they are written,
- * by the rule of the swap records (a group is group_size channels of one token of one KV head; see the record format above; the
- * scale is (max x - min x) times the binary32 number next to 1 / (2^b - 1), so that where the quotient lies half-way between two
- * fp16 numbers it may be the other one), and attention reads the codes.  `desc` gives the pool's shape as above (n_tokens = slots * chunk_len; quant_mode 0; the strides are
+ * and attention reads the codes.  A group is group_size channels of one token of one KV head.  In binary32 with every step rounded to
+ * nearest, and r the binary32 number next to 1 / (2^b - 1):
+ *     zero = min x (+0 when it is a zero);  scale = fp16((max x - min x) * r);
+ *     code = min(2^b - 1, rint((x - zero) * (1 / scale)))  (ties to even; all codes 0 when scale == 0);  held value = zero + code * scale.
+ * That is the swap records' rule but for the scale, there a quotient by 2^b - 1.  The scale is the record's, or, where the quotient lies
+ * within 2^-22 of half-way between two fp16 numbers, it may be the next fp16 number above it (r is above 1 / (2^b - 1) at 4 and 8 bits);
+ * the group's codes may differ then too.  Neither scale is nearer.  So a held group is not to be taken for its record bit by bit.
+ * `desc` gives the pool's shape as above (n_tokens = slots * chunk_len; quant_mode 0; the strides are
  * checked but have no influence) and `bits` (4 or 8) the width of its codes.  A held pool is llms_held_bytes(desc, bits) bytes,
  *     [n_layers][n_kv_heads][tile][K codes | V codes | K parameters | V parameters],
  * a tile being 16 consecutive rows of the pool.  Parameters: [token][group] of {u16 scale, u16 zero-point} (fp16 bits).  With

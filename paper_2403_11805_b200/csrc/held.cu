@@ -1,7 +1,7 @@
 // Quantising K and V rows into a pool held at 8 or 4 bits, and reading rows back out of it.
 //
-// Mathematics.  Per group of channels of a token: zero = min x, scale = fp16((max x - min x) / (2^b - 1)), code = rint((x - zero) / scale);
-// the group stands for zero + code * scale.
+// Mathematics.  Per group of channels of a token: zero = min x, scale = fp16((max x - min x) * r) with r next to 1 / (2^b - 1), code =
+// rint((x - zero) * (1 / scale)); the group stands for zero + code * scale.
 //
 // Bound.  Every element is read and written once (2 bytes one way, b / 8 and its share of the parameters the other), with some ten
 // instructions in between: memory-bound.

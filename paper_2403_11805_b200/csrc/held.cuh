@@ -106,8 +106,9 @@ struct GroupRange {
     }
 };
 
-// Scale and zero-point of a group and what its codes are made with; the rule is the swap records' (binary32, to nearest, nothing
-// fused), but for the scale, which is a product with 1 / (2^b - 1) instead of a quotient.
+// Scale and zero-point of a group and what its codes are made with: binary32, to nearest, nothing fused.  The scale is a product with
+// the binary32 number next to 1 / TOP, which lies above 1 / TOP for 15 and 255.  So where the quotient, which the swap records take,
+// lies half-way between two fp16 numbers the scale is the upper of the two, and a record's the even one; elsewhere they are the same.
 struct GroupRule {
     float zero, inverse, scale;                   // a group with an infinity or a NaN: zero is NaN, all codes are 0
     uint32_t params;                              // (scale, zero) in fp16
