@@ -205,7 +205,8 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_write_kernel(const HeldR
     const int span = a.by_heads(unit), h = unit - span * a.H;
     HeldSpan s;
     if (span >= a.spans || !find_span(a, span, s)) return;
-    uint8_t *tile = s.tile < 0 ? nullptr : a.held + ((int64_t)h * a.tiles + s.tile) * S::kTileBytes;
+    const bool stored = s.tile >= 0;                          // (else no pointer into the tile is used)
+    uint8_t *const tile = a.held + ((int64_t)h * a.tiles + max(s.tile, (int64_t)0)) * S::kTileBytes;
     const int g = lane >> 2, j = lane & 3;
     constexpr int kWordChannels = 32 / S::BITS, kUnitChannels = 16 / S::BITS;
     uint32_t k[2][S::W][kWordChannels / 2], v[2][2][S::W][kUnitChannels / 2];  // tokens 8 i + g of K; 8 i + 2 j + e of V
@@ -228,11 +229,11 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_write_kernel(const HeldR
         const bool has = s.has(t);
         uint32_t code[S::W];
         if (!s.any(i)) continue;                              // (one new token: most of the tile is somebody else's)
-        encode_token<S, BF, SEEN, kWordChannels, 1, 4>(k[i], code, has, tile != nullptr, reinterpret_cast<uint32_t *>(tile + 2 * S::kCodes) + t * S::GPR,
-                                                       tile && has && j == 0,
+        encode_token<S, BF, SEEN, kWordChannels, 1, 4>(k[i], code, has, stored, reinterpret_cast<uint32_t *>(tile + 2 * S::kCodes) + t * S::GPR,
+                                                       stored && has && j == 0,
                                                        SEEN ? a.k_out + (s.row0 + t) * a.out_stride + (int64_t)h * S::D + j * kWordChannels : nullptr,
                                                        4 * kWordChannels);
-        if (tile && has) {
+        if (stored && has) {
 #pragma unroll
             for (int w = 0; w < S::W; w += S::VW) {
                 uint32_t x[S::VW];
@@ -248,13 +249,13 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_write_kernel(const HeldR
         const int t = 8 * i + 2 * j;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-            if (s.any(i, e)) encode_token<S, BF, SEEN, kUnitChannels, 4, 32>(v[i][e], code[e], s.has(t + e), tile != nullptr,
+            if (s.any(i, e)) encode_token<S, BF, SEEN, kUnitChannels, 4, 32>(v[i][e], code[e], s.has(t + e), stored,
                                                             reinterpret_cast<uint32_t *>(tile + 2 * S::kCodes + S::kParams) + (t + e) * S::GPR,
-                                                            tile && s.has(t + e) && g == 0,
+                                                            stored && s.has(t + e) && g == 0,
                                                             SEEN ? a.v_out + (s.row0 + t + e) * a.out_stride + (int64_t)h * S::D + g * kUnitChannels : nullptr,
                                                             8 * kUnitChannels);
         uint32_t *codes = reinterpret_cast<uint32_t *>(tile + S::kCodes);
-        if (tile && s.has(t) && s.has(t + 1)) {
+        if (stored && s.has(t) && s.has(t + 1)) {
 #pragma unroll
             for (int w = 0; w < S::W; w += S::VW) {
                 uint32_t x[S::VW];
@@ -262,7 +263,7 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_write_kernel(const HeldR
                 for (int n = 0; n < S::VW; ++n) x[n] = __byte_perm(code[0][w + n], code[1][w + n], 0x5410);
                 store_words(codes + S::place(i, w, lane), x);
             }
-        } else if (tile && (s.has(t) || s.has(t + 1))) {      // the other token's half of the words stays
+        } else if (stored && (s.has(t) || s.has(t + 1))) {      // the other token's half of the words stays
             const int e = s.has(t) ? 0 : 1;
 #pragma unroll
             for (int w = 0; w < S::W; ++w) reinterpret_cast<uint16_t *>(codes + S::place(i, w, lane))[e] = (uint16_t)(e ? code[1][w] : code[0][w]);
@@ -293,7 +294,8 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_read_kernel(const HeldRo
     const int span = a.by_heads(unit), h = unit - span * a.H;
     HeldSpan s;
     if (span >= a.spans || !find_span(a, span, s)) return;
-    const uint8_t *tile = s.tile < 0 ? nullptr : a.held + ((int64_t)h * a.tiles + s.tile) * S::kTileBytes;
+    // (an address, 0 if the tokens lie nowhere: what is added to it then is no pointer)
+    const uintptr_t tile = s.tile < 0 ? 0 : reinterpret_cast<uintptr_t>(a.held + ((int64_t)h * a.tiles + s.tile) * S::kTileBytes);
     const int g = lane >> 2, j = lane & 3;
     constexpr int kWordChannels = 32 / S::BITS, kUnitChannels = 16 / S::BITS;
     uint32_t x[2][2][S::W], k_rule[2][S::GPR], v_rule[2][2][S::GPR];           // [K, V][i]; of tokens 8 i + g; of tokens 8 i + 2 j + e
@@ -304,18 +306,18 @@ __global__ void __launch_bounds__(kHeldWarps * 32) held_read_kernel(const HeldRo
 #pragma unroll
             for (int w = 0; w < S::W; w += S::VW) {
                 uint32_t v[S::VW];
-                load_words_if<false>(tile != nullptr, v, reinterpret_cast<const uint32_t *>(tile + half * S::kCodes) + S::place(i, w, lane));
+                load_words_if<false>(tile != 0, v, reinterpret_cast<const uint32_t *>(tile + half * S::kCodes + S::place(i, w, lane) * 4));
 #pragma unroll
                 for (int n = 0; n < S::VW; ++n) x[half][i][w + n] = v[n];
             }
-    const uint32_t *const rules = reinterpret_cast<const uint32_t *>(tile + 2 * S::kCodes);
+    auto rule_of = [&](int i) { return tile ? __ldg(reinterpret_cast<const uint32_t *>(tile + 2 * S::kCodes + i * 4)) : kNanHalf << 16; };
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int grp = 0; grp < S::GPR; ++grp) {
-            k_rule[i][grp] = tile ? __ldg(rules + (8 * i + g) * S::GPR + grp) : kNanHalf << 16;
+            k_rule[i][grp] = rule_of((8 * i + g) * S::GPR + grp);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) v_rule[i][e][grp] = tile ? __ldg(rules + 16 * S::GPR + (8 * i + 2 * j + e) * S::GPR + grp) : kNanHalf << 16;
+            for (int e = 0; e < 2; ++e) v_rule[i][e][grp] = rule_of((16 + 8 * i + 2 * j + e) * S::GPR + grp);
         }
     uint16_t *const k_to = a.k_out + (int64_t)h * S::D + j * kWordChannels, *const v_to = a.v_out + (int64_t)h * S::D + g * kUnitChannels;
 #pragma unroll

@@ -257,9 +257,9 @@ __device__ __forceinline__ void join_parts(const DecodeArgs &a, bool bf16, const
 constexpr int kItemSlots = 5;
 struct HeldCut {
     int w0, w1;                                   // the run's tiles, in the batch's numbering
-    int seq, base, slot;                          // the sequence of the first one, the numbers of its first tile and of its first slot
+    int seq = 0, base = 0, slot = 0;              // the sequence of the first one, the numbers of its first tile and of its first slot
     int total;                                    // slots
-    SeqTiles s;
+    SeqTiles s{};                                 // (a run behind the last slot has no tiles, and none of these)
     __device__ __forceinline__ HeldCut(const DecodeArgs &a, int run, int lane)
     {
         const int per_seq = a.Hkv * a.blocks, each = (a.n_seqs + 31) / 32;
