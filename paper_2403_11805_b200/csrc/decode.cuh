@@ -1,12 +1,11 @@
-// What the kernels that attend to a paged cache share: the batch's tiles and how they are handed out, online softmax, joining of
-// partial results, weights.  decode.cu has the mathematics and the split.
+// What the kernels that attend to a paged cache share (decode.cu, held_attention.cuh): operands, the batch's tiles and runs of them, conversions,
+// how a row ends, the workspace and when a call has clusters.  decode.cu has the mathematics and the split.
 #pragma once
 
 #include <math.h>
 
 #include <algorithm>
 
-#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include "paged.cuh"
@@ -14,10 +13,7 @@
 
 namespace llms {
 
-namespace cg = cooperative_groups;
-
 constexpr int kTile = 16;                         // tokens per tile: the 16 side of an MMA
-constexpr int kQuerySlots = 2;                    // items whose query rows a warp holds: the current one's, the next one's
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Weights are taken against a reference that follows the running maximum in steps: it moves only when a logit exceeds it by more
 // than kSlack (in units of log2), so most tiles need no maximum over the warp's lanes and no rescaling.
@@ -88,39 +84,11 @@ struct Runs {
     }
 };
 
-// Wait for the phase of the given parity to complete, all lanes of a warp together; false when it did not within the limit.
-__device__ __forceinline__ bool warp_wait(unsigned long long *bar, uint32_t parity)
-{
-    const uint32_t addr = smem_u32(bar);
-    uint32_t done = 0;
-    for (uint32_t i = 0; i < kSpinLimit; ++i) {
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-                     : "=r"(done) : "r"(addr), "r"(parity) : "memory");
-        if (done) break;
-        if (i > 32) __nanosleep(64);
-    }
-    return __all_sync(0xffffffffu, done);
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, unsigned long long *bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 :: "r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
-}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
 {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
-}
-template <bool BF>
-__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    if constexpr (BF)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float exp2_fast(float x)
 {
@@ -178,19 +146,6 @@ template <int DB> struct DecodeCols {
     static constexpr int kPitch = kCols + 4;                  // floats per row of a partial result: O, then m and l
 };
 
-constexpr int kItemWarps = 4;
-
-// In a cluster, the first of n tiles that its warp number i takes.
-template <int W>
-__device__ __forceinline__ int part_begin(const DecodeArgs &a, int n, int i) { return (n * i) >> (a.item_shift + (W == 4 ? 2 : 0)); }
-
-__device__ __forceinline__ void lse_add(float &top, float &sum, float m, float l)   // (top, sum) joined with (m, l)
-{
-    const float t = fmaxf(top, m), ref = t == -INFINITY ? 0.0f : t;
-    sum = __fmaf_rn(sum, exp2_fast(top - ref), l * exp2_fast(m - ref));
-    top = t;
-}
-
 // Rows without tokens: zeros, or NaN where the length is invalid.
 template <bool BF>
 __device__ __forceinline__ void fill_empty(const DecodeArgs &a, int64_t row, int rows, bool bad, int tid, int threads)
@@ -202,343 +157,6 @@ __device__ __forceinline__ void fill_empty(const DecodeArgs &a, int64_t row, int
 #pragma unroll 1
     for (int i = tid; i < rows; i += threads)
         if (a.lse) a.lse[row + i] = bad ? NAN : -INFINITY;
-}
-
-// The end of an item that a cluster has: the warps' pieces joined, each CTA taking an equal share of the row elements, and the
-// weights of the warp's own tokens [16 w0, 16 w1).
-template <bool BF, int DB, int NT>
-__device__ __forceinline__ void join_item(const DecodeArgs &a, unsigned char *rings, int warp_bytes, int w0, int w1)
-{
-    using S = DecodeCols<DB>;
-    constexpr int W = kItemWarps, kThreads = W * 32;
-    __shared__ float s_factor[8 * NT * W], s_lse[W][8 * NT];
-    __shared__ float2 s_joined[8 * NT];
-    __shared__ int s_piece;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int ctas = 1 << a.item_shift, part = blockIdx.x & (ctas - 1), item = blockIdx.x >> a.item_shift;
-    const int per_seq = a.Hkv * a.blocks, b = a.by_per_seq(item), hb = item - b * per_seq, h = a.by_blocks(hb), row0 = (hb - h * a.blocks) * 8 * NT;
-    const int have = min(a.rows, a.group - row0), len = __ldg(a.lens + b);
-    const int64_t first_row = (int64_t)b * a.Hq + h * a.group + row0;
-    const SeqTiles s = seq_tiles(a, len);
-    if (s.n == 0) {
-        if (part == 0) fill_empty<BF>(a, first_row, have, len != 0, tid, kThreads);
-        return;
-    }
-    // the CTA's own pieces first, into the first live warp's place; then, through the cluster's shared memory, the CTAs' pieces
-    auto local = [&](int w) { return reinterpret_cast<float *>(rings + w * warp_bytes); };
-    const int mine0 = part * W;
-    int first = 0;
-    while (first < W && part_begin<W>(a, s.n, mine0 + first) == part_begin<W>(a, s.n, mine0 + first + 1)) ++first;
-    __syncthreads();
-    if (first < W - 1) {
-#pragma unroll 1
-        for (int e = tid; e < have * W; e += kThreads) {       // factor of every piece's row
-            const int r = e / W, w = e - r * W;
-            float top = -INFINITY, m = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                if (part_begin<W>(a, s.n, mine0 + i) == part_begin<W>(a, s.n, mine0 + i + 1)) continue;
-                const float2 ml = *reinterpret_cast<const float2 *>(local(i) + r * S::kPitch + S::kCols);
-                lse_add(top, sum, ml.x, ml.y);
-                if (i == w) m = ml.x;
-            }
-            s_factor[r * W + w] = exp2_fast(m - (top == -INFINITY ? 0.0f : top));
-            if (w == 0) s_joined[r] = make_float2(top, sum);
-        }
-        __syncthreads();
-#pragma unroll 1
-        for (int e = tid; e < have * (S::kCols / 4); e += kThreads) {
-            const int r = e / (S::kCols / 4), c = (e - r * (S::kCols / 4)) * 4;
-            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                if (part_begin<W>(a, s.n, mine0 + i) == part_begin<W>(a, s.n, mine0 + i + 1)) continue;
-                const float f = s_factor[r * W + i];
-                const float4 v = *reinterpret_cast<const float4 *>(local(i) + r * S::kPitch + c);
-                acc.x = __fmaf_rn(f, v.x, acc.x);
-                acc.y = __fmaf_rn(f, v.y, acc.y);
-                acc.z = __fmaf_rn(f, v.z, acc.z);
-                acc.w = __fmaf_rn(f, v.w, acc.w);
-            }
-            *reinterpret_cast<float4 *>(local(first) + r * S::kPitch + c) = acc;   // only this thread reads or writes these elements
-        }
-        __syncthreads();
-        for (int r = tid; r < have; r += kThreads) *reinterpret_cast<float2 *>(local(first) + r * S::kPitch + S::kCols) = s_joined[r];
-    }
-    if (tid == 0) s_piece = first < W ? first * warp_bytes : -1;
-    cluster.sync();
-    int at_cta[8];                                            // where a CTA's piece lies, -1: it has none
-#pragma unroll
-    for (int i = 0; i < 8; ++i) at_cta[i] = i < ctas ? *cluster.map_shared_rank(&s_piece, i) : -1;
-    auto piece = [&](int i) -> const float * { return reinterpret_cast<const float *>(cluster.map_shared_rank(rings, i) + at_cta[i]); };
-    const int share = (a.rows * (S::kCols / 4)) >> a.item_shift;               // groups of four channels that this CTA joins
-#pragma unroll 1
-    for (int e = part * share + tid; e < (part + 1) * share; e += kThreads) {
-        const int r = e / (S::kCols / 4), c = (e - r * (S::kCols / 4)) * 4;
-        if (r >= have) continue;
-        float2 ml[8];
-        float4 v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            ml[i] = make_float2(-INFINITY, 0.0f);
-            v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (at_cta[i] >= 0) {
-                ml[i] = *reinterpret_cast<const float2 *>(piece(i) + r * S::kPitch + S::kCols);
-                v[i] = *reinterpret_cast<const float4 *>(piece(i) + r * S::kPitch + c);
-            }
-        }
-        float top = -INFINITY, sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
-        const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float w = exp2_fast(ml[i].x - ref);
-            sum = __fmaf_rn(w, ml[i].y, sum);
-            acc[0] = __fmaf_rn(w, v[i].x, acc[0]);
-            acc[1] = __fmaf_rn(w, v[i].y, acc[1]);
-            acc[2] = __fmaf_rn(w, v[i].z, acc[2]);
-            acc[3] = __fmaf_rn(w, v[i].w, acc[3]);
-        }
-        finish_row<BF>(a, first_row + r, c, acc, top, sum);
-    }
-    if (a.mass_out) {                                         // (only where an item has all query heads of its KV head)
-        for (int r = lane; r < have; r += 32) {
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (at_cta[i] >= 0) {
-                    const float2 ml = *reinterpret_cast<const float2 *>(piece(i) + r * S::kPitch + S::kCols);
-                    lse_add(top, sum, ml.x, ml.y);
-                }
-            s_lse[warp][r] = sum == 0.0f ? -INFINITY : top + log2f(sum);
-        }
-        __syncwarp();
-        const int64_t at = (int64_t)b * a.Hkv + h;
-        const float *v = a.logits + at * a.max_len * a.group, *in = a.mass_in ? a.mass_in + at * a.mass_stride : nullptr;
-        float *out = a.mass_out + at * a.mass_stride;
-        const int t1 = min(s.len, (s.tile0 + w1) * kTile);
-        constexpr int kAtOnce = 4;                            // tokens of a lane whose loads are under way together
-        auto put = [&](int t0, int end, int step, auto weight) {               // tokens t0, t0 + step, ...
-#pragma unroll 1
-            for (int t = t0; t < end; t += kAtOnce * step) {
-                float w[kAtOnce];
-#pragma unroll
-                for (int i = 0; i < kAtOnce; ++i) {
-                    const int u = t + i * step;
-                    w[i] = u < end ? weight(u) : 0.0f;
-                    if (in && u < end) w[i] = in[u] + w[i];
-                }
-#pragma unroll
-                for (int i = 0; i < kAtOnce; ++i)
-                    if (t + i * step < end) out[t + i * step] = w[i];
-            }
-        };
-        auto one = [&](float x, int r) { return s_lse[warp][r] == -INFINITY ? 0.0f : exp2_fast(x - s_lse[warp][r]); };
-        put(max(s.first, (s.tile0 + w0) * kTile) + lane, t1, 32, [&](int t) {
-            const float *x = v + (int64_t)t * a.group;
-            float w = 0.0f;
-            if ((have & 3) == 0) {                            // (have is the group here)
-                for (int r = 0; r < have; r += 4) {
-                    const float4 y = *reinterpret_cast<const float4 *>(x + r);
-                    w += (one(y.x, r) + one(y.y, r + 1)) + (one(y.z, r + 2) + one(y.w, r + 3));
-                }
-            } else {
-                for (int r = 0; r < have; ++r) w += one(x[r], r);
-            }
-            return w;
-        });
-        if (in != out) put(part * kThreads + tid, s.first, ctas * kThreads, [&](int) { return 0.0f; });   // before the window
-    }
-    cluster.sync();                                           // nobody reads this CTA's pieces any more
-}
-
-// The tiles [w0, w1) of a warp, and a sequence at or before the first of them with the number of its first tile.
-template <bool ITEM, int W>
-__device__ __forceinline__ void find_tiles(const DecodeArgs &a, int warp, int lane, int &w0, int &w1, int &f_seq, int &f_base, int &total, SeqTiles &f_s)
-{
-    const int run = blockIdx.x, per_seq = a.Hkv * a.blocks;
-    total = 0;
-    if constexpr (ITEM) {
-        // the item of the cluster, its tiles numbered from 0, and this warp's part of them
-        const int item = run >> a.item_shift, me = (run & ((1 << a.item_shift) - 1)) * W + warp;
-        f_seq = a.by_per_seq(item);
-        f_s = seq_tiles(a, __ldg(a.lens + f_seq));
-        f_base = -(item - f_seq * per_seq) * f_s.n;
-        w0 = part_begin<W>(a, f_s.n, me);
-        w1 = part_begin<W>(a, f_s.n, me + 1);
-    } else {
-        // tiles of the batch, and the sequence that this run begins in: a lane adds up neighbouring sequences
-        const int each = (a.n_seqs + 31) / 32;
-        int incl = 0;
-        for (int b = lane * each; b < min(a.n_seqs, (lane + 1) * each); ++b) incl += seq_tiles(a, __ldg(a.lens + b)).n * per_seq;
-        const int own = incl;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int up = __shfl_up_sync(0xffffffffu, incl, d);
-            if (lane >= d) incl += up;
-        }
-        total = __shfl_sync(0xffffffffu, incl, 31);
-        const Runs cut(a, total);
-        w0 = run < cut.n ? cut.begin(run) : 0;
-        w1 = run < cut.n ? cut.begin(run + 1) : 0;
-        const int holder = max(0, __ffs(__ballot_sync(0xffffffffu, incl > w0)) - 1);
-        f_seq = holder * each;
-        f_base = __shfl_sync(0xffffffffu, incl - own, holder);
-        f_s = seq_tiles(a, __ldg(a.lens + f_seq));
-    }
-}
-
-// Items that span runs are joined, block (x, y) taking kJoinCols groups of four channels of the y-th part of item x (by_item) or of
-// the item that is open at the end of run x, in SLICES over the runs that have pieces of it.  The other blocks: the weights
-// of kMassTokens tokens per thread.
-constexpr int kJoinCols = 16, kMassTokens = 2;
-struct FinishArgs {
-    int by_item, joins, join_y, cols, mass_x;
-};
-
-template <bool BF, int SLICES>
-__global__ void __launch_bounds__(SLICES * kJoinCols) finish_kernel(const DecodeArgs a, const FinishArgs f)
-{
-    constexpr int kThreads = SLICES * kJoinCols;
-    __shared__ float4 s_acc[kThreads];
-    __shared__ float2 s_ml[SLICES];
-    __shared__ float s_lse[64];
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const int per_seq = a.Hkv * a.blocks, pitch = f.cols + 4, block_rows = a.group > 8 ? 16 : 8;
-    const int64_t stride = (int64_t)a.rows * pitch;
-    if ((int)blockIdx.x < f.joins) {
-        const int x = blockIdx.x / f.join_y, y = blockIdx.x - x * f.join_y;
-        const int item = f.by_item ? x : a.open[x];
-        if (item < 0) return;
-        const int b = a.by_per_seq(item), hb = item - b * per_seq, h = a.by_blocks(hb), rb = hb - h * a.blocks;
-        const int2 span = a.span[item];
-        if (f.by_item && seq_tiles(a, __ldg(a.lens + b)).n == 0) return;   // its span was never written
-        if (span.x < 0) return;
-        const int slice = threadIdx.x / kJoinCols, e = y * kJoinCols + threadIdx.x % kJoinCols;
-        const int r = e / (f.cols / 4), c = (e - r * (f.cols / 4)) * 4;     // one row per block: cols / 4 is a multiple of kJoinCols
-        if (rb * block_rows + r >= a.group) return;
-        float top = -INFINITY, sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        const float *from = a.part + (int64_t)r * pitch;
-#pragma unroll 4
-        for (int i = span.x + slice; i <= span.y; i += SLICES) {
-            // the first run's last piece, then the following runs' first ones
-            const float *at = from + ((int64_t)i * 2 + (i == span.x)) * stride;
-            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(at + f.cols));
-            const float4 v = __ldcg(reinterpret_cast<const float4 *>(at + c));
-            const float t = fmaxf(top, ml.x), ref = t == -INFINITY ? 0.0f : t;
-            const float keep = exp2_fast(top - ref), w = exp2_fast(ml.x - ref);
-            top = t;
-            sum = __fmaf_rn(sum, keep, w * ml.y);
-            acc[0] = __fmaf_rn(acc[0], keep, w * v.x);
-            acc[1] = __fmaf_rn(acc[1], keep, w * v.y);
-            acc[2] = __fmaf_rn(acc[2], keep, w * v.z);
-            acc[3] = __fmaf_rn(acc[3], keep, w * v.w);
-        }
-        s_acc[threadIdx.x] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-        if (threadIdx.x % kJoinCols == 0) s_ml[slice] = make_float2(top, sum);
-        __syncthreads();
-        if (slice) return;
-        const int n = min(SLICES, span.y - span.x + 1);
-        for (int i = 1; i < n; ++i) top = fmaxf(top, s_ml[i].x);
-        const float ref = top == -INFINITY ? 0.0f : top;
-        sum = acc[0] = acc[1] = acc[2] = acc[3] = 0.0f;
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const float2 ml = s_ml[i];
-            const float4 v = s_acc[i * kJoinCols + threadIdx.x];
-            const float w = exp2_fast(ml.x - ref);
-            sum = __fmaf_rn(w, ml.y, sum);
-            acc[0] = __fmaf_rn(w, v.x, acc[0]);
-            acc[1] = __fmaf_rn(w, v.y, acc[1]);
-            acc[2] = __fmaf_rn(w, v.z, acc[2]);
-            acc[3] = __fmaf_rn(w, v.w, acc[3]);
-        }
-        finish_row<BF>(a, (int64_t)b * a.Hq + h * a.group + rb * block_rows + r, c, acc, top, sum);
-        return;
-    }
-    // weights: 2^(v - lse) over the query heads of the KV head
-    const int x = blockIdx.x - f.joins;
-    const int bh = a.by_mass_x(x), b = a.by_hkv(bh), h = bh - b * a.Hkv, t0 = (x - bh * f.mass_x) * kThreads * kMassTokens, len = __ldg(a.lens + b);
-    if (len > a.max_len || t0 >= len) return;
-    const int first = a.window > 0 && len > a.window ? len - a.window : 0;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t at = (int64_t)b * a.Hkv + h;
-    const float *v = a.logits + at * a.max_len * a.group;
-    float w[kMassTokens], before[kMassTokens];                // added once, at the end: one rounding at the size of the mass
-    float4 early[kMassTokens];                                // the logits, where a token has four: asked for before the log-sums
-    int t[kMassTokens];
-    const bool four = a.group == 4;
-#pragma unroll
-    for (int j = 0; j < kMassTokens; ++j) {
-        t[j] = t0 + j * kThreads + threadIdx.x;
-        w[j] = 0.0f;
-        before[j] = a.mass_in && t[j] < len ? a.mass_in[at * a.mass_stride + t[j]] : 0.0f;
-        if (four && t[j] < len && t[j] >= first) early[j] = __ldcg(reinterpret_cast<const float4 *>(v) + t[j]);
-    }
-    for (int g0 = 0; g0 < a.group; g0 += 64) {
-        const int n_g = min(64, a.group - g0);
-        for (int g = warp; g < n_g; g += kThreads / 32) {
-            const int rb = (g0 + g) / block_rows, r = g0 + g - rb * block_rows;
-            const int2 span = a.span[b * per_seq + h * a.blocks + rb];
-            float lse;
-            if (span.x < 0) {
-                lse = a.row_lse[at * a.group + g0 + g];
-            } else {                                          // the joining blocks run at the same time: again from the pieces
-                float top = -INFINITY, sum = 0.0f;
-                const float *from = a.part + (int64_t)r * pitch + f.cols;
-#pragma unroll 4
-                for (int i = span.x + lane; i <= span.y; i += 32) {
-                    const float2 ml = __ldcg(reinterpret_cast<const float2 *>(from + ((int64_t)i * 2 + (i == span.x)) * stride));
-                    lse_add(top, sum, ml.x, ml.y);
-                }
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const float m2 = __shfl_xor_sync(0xffffffffu, top, d), l2 = __shfl_xor_sync(0xffffffffu, sum, d);
-                    lse_add(top, sum, m2, l2);
-                }
-                lse = sum == 0.0f ? -INFINITY : top + log2f(sum);
-            }
-            if (lane == 0) s_lse[g] = lse;
-        }
-        __syncthreads();
-        auto weight = [&](float x, float lse) { return lse == -INFINITY ? 0.0f : exp2_fast(x - lse); };
-        if (four) {
-#pragma unroll
-            for (int j = 0; j < kMassTokens; ++j)
-                if (t[j] < len && t[j] >= first)
-                    w[j] = (weight(early[j].x, s_lse[0]) + weight(early[j].y, s_lse[1])) + (weight(early[j].z, s_lse[2]) + weight(early[j].w, s_lse[3]));
-        } else {
-            for (int g = 0; g < n_g; ++g)
-#pragma unroll
-                for (int j = 0; j < kMassTokens; ++j)
-                    if (t[j] < len && t[j] >= first) w[j] += weight(__ldcg(v + (int64_t)t[j] * a.group + g0 + g), s_lse[g]);
-        }
-        __syncthreads();
-    }
-#pragma unroll
-    for (int j = 0; j < kMassTokens; ++j)
-        if (t[j] < len) a.mass_out[at * a.mass_stride + t[j]] = before[j] + w[j];
-}
-
-template <bool BF>
-int launch_finish(DecodeArgs &a, FinishArgs f, cudaStream_t st)
-{
-    // few items: a block per item and part of its row, the slices as many as its pieces call for; more items than runs: a block
-    // per run, whose open item has pieces in few other runs
-    const int n_items = a.n_seqs * a.Hkv * a.blocks, slices = a.grid_runs >= 128 * n_items ? 64 : (a.grid_runs >= 16 * n_items ? 16 : 4);
-    f.by_item = n_items <= a.grid_runs;
-    f.join_y = a.rows * (f.cols / 4) / kJoinCols;
-    f.joins = std::min(n_items, a.grid_runs) * f.join_y;
-    const int tokens = slices * kJoinCols * kMassTokens;
-    f.mass_x = (a.max_len + tokens - 1) / tokens;
-    a.by_mass_x = Divisor(f.mass_x);
-    const dim3 grid(f.joins + (a.mass_out ? f.mass_x * a.Hkv * a.n_seqs : 0)), block(slices * kJoinCols);
-    LLMS_CUDA_TRY(launch_dependent(slices == 64 ? finish_kernel<BF, 64> : (slices == 16 ? finish_kernel<BF, 16> : finish_kernel<BF, 4>),
-                                   grid, block, 0, st, a, f));
-    return LLMS_OK;
 }
 
 constexpr int kRounds = 4, kRunTiles = 16;
@@ -598,11 +216,10 @@ inline void set_decode_shape(DecodeArgs &a, const llms_kv_desc &d, const DecodeL
     a.q_bytes = a.rows * a.d * 2;
 }
 
-// CTAs of a cluster per item, or 0: runs.  As many CTAs as leave a warp one tile, up to eight and up to kItemRounds rounds of the
+// CTAs of a cluster per item, or 0: runs.  As many CTAs as leave a warp one tile, up to eight and up to `rounds` rounds of the
 // GPU (per_sm: CTAs that an SM has room for); not if a warp is left with more than four tiles, in a batch (whose sequences are
 // seldom all as long as max_len) eight.
-constexpr int kItemRounds = 2;
-inline int decode_item_ctas(const DecodeArgs &a, int per_sm, int rounds = kItemRounds, int tile = kTile, int warps = kItemWarps)
+inline int decode_item_ctas(const DecodeArgs &a, int per_sm, int rounds, int tile, int warps)
 {
     if (a.mass_out && a.blocks > 1) return 0;                 // a token's weight is made of several items' logits
     const int seen = a.window > 0 ? (int)std::min<int64_t>(a.max_len, (int64_t)a.window + tile - 1) : a.max_len, tiles = (seen + tile - 1) / tile;
