@@ -399,7 +399,9 @@ int llms_held_read(const llms_kv_desc *desc, int bits, int dtype, int layer, con
  * sees them as they are held.  Sums are kept in binary32.  All arguments and results as there, without masses; dtype is that of
  * q, k_new, v_new and out.  A query row with an infinity or a NaN gives NaN.
  * The products with V take a token's weight times its scale as a pair of 16-bit values: off by less than 2^-20 of it, and by up to
- * 2^-29 of the row's largest weight times its largest scale, which smaller products lose.
+ * 2^-29 of the row's largest weight times its largest scale, which smaller products lose.  Both products' sums are cut off, not rounded, to
+ * binary32 or a little less.  Values of bfloat16 queries below 2^-29 of their row's largest may be rounded, to a multiple of at most
+ * 2^-38 of it.
  *   workspace device, 256-byte aligned, llms_held_workspace_bytes(desc, bits, n_seqs, max_len); may be reused by the next call on the
  *             same stream */
 int llms_held_workspace_bytes(const llms_kv_desc *desc, int bits, int n_seqs, int max_len, uint64_t *nbytes);

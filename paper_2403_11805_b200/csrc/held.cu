@@ -4,7 +4,8 @@
 // rint((x - zero) * (1 / scale)); the group stands for zero + code * scale.
 //
 // Bound.  Every element is read and written once (2 bytes one way, b / 8 and its share of the parameters the other), with some ten
-// instructions in between: memory-bound.
+// instructions in between.  Memory would bound it; what does is how many loads are under way, which for a write are the rows that
+// 96 registers and five warps per scheduler hold (2.3 stalled cycles per instruction on loads, 60% of the issue slots busy).
 //
 // Split.  A warp takes K and V of one KV head's 16 tokens of one sequence: a tile of the pool, in whose order of codes its lanes hold the
 // channels from the start, so that a whole tile is written (or read) in full vectors and nothing is exchanged but the ranges
@@ -12,9 +13,9 @@
 // a tile: the other tokens' codes in it are left as they are.  Neighbouring warps take the heads of the same tokens, whose
 // rows lie side by side.
 //
-// Measured, a B200, 4 bits: a prompt of 32768 tokens, 8 heads of 128 channels, written in 34 to 36 us (170 MB, 4.7 to 4.9 TB/s; 11
-// instructions per channel: 60% of the issue slots); 4096 tokens of 32 heads read in 16.2 us (85 MB, 5.2 TB/s); one token for each of
-// 32 sequences, one head of 256 channels at 8 bits, 5.2 us.  K and V in warps of their own: 55 and 22 us.
+// Measured, a B200, 4 bits: a prompt of 32768 tokens, 8 heads of 128 channels, written in 35 us (170 MB, 4.8 TB/s; 11
+// instructions per channel); 4096 tokens of 32 heads read in 16.3 us (85 MB, 5.2 TB/s); one token for each of
+// 32 sequences, one head of 256 channels at 8 bits, 4.3 us.  K and V in warps of their own: 55 and 22 us.
 #include <algorithm>
 #include <type_traits>
 

@@ -9,8 +9,9 @@
 //
 // Bound.  A quarter (half) of the fp16 pool's bytes for the same arithmetic: at 4 bits and 128 channels an SM has some 80 cycles per 16
 // tokens at the copy bandwidth, in which its four schedulers issue at most 320 instructions; 16 tokens take 250, half of
-// them logical ones that hold their pipe for two cycles.  So it is the arithmetic that bounds large batches (without its copies
-// the kernel takes the same time), and the latencies of length, table, tile and join that bound small calls.
+// them logical ones that hold their pipe for two cycles.  Large batches take the same time without their copies, with 55% of the
+// issue slots and half of that pipe busy: the fixed latencies of a warp's chain of instructions bound them, at four warps per scheduler.
+// The latencies of length, table, tile and join bound small calls.
 //
 // Split.  As for the fp16 pool: runs of tiles, one per warp, or a cluster per item for small calls.  A tile of the pool is one run of bytes,
 // copied by a warp's own lanes (cp.async: a third of the instructions that one lane's bulk copies and their barriers took), and
@@ -18,8 +19,9 @@
 // parts of a cluster's warps are stored into the shared memory of the CTA that joins them: one barrier, no reads across.
 //
 // Measured, a B200: 16 contexts of 4096 tokens, 32 heads of 128 channels at 4 bits 64 us (286 MB, 4.5 TB/s; 164 us in the fp16 pool); one
-// grouped-query context of 32768 tokens 20.3 us; one context of 4096 tokens 10.9; one of 256 tokens, 4 heads of 64, 4.2.
-// Warps per SM for the batch: 12 72 us, 16 64, 20 66 (96 registers: spills).
+// grouped-query context of 32768 tokens 19.8 us; one context of 4096 tokens 10.3; one of 256 tokens, 4 heads of 64, 4.1.
+// Warps per SM (us for 12, 16, 20, the last at 96 registers with spills): that batch 68, 64, 64; 64 contexts 226, 216, 220; 64
+// contexts of 8 heads with four query rows 82, 78, 86.
 #pragma once
 
 #include "decode.cuh"
