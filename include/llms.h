@@ -398,7 +398,7 @@ int llms_held_read(const llms_kv_desc *desc, int bits, int dtype, int layer, con
  * unrounded), one layer.  k_new and v_new, if given, are quantised into the pool as token lens[b] - 1 by the same call, which then
  * sees them as they are held.  Sums are kept in binary32.  All arguments and results as there, without masses; dtype is that of
  * q, k_new, v_new and out.  A query row with an infinity or a NaN gives NaN.
- * The products with V take a token's weight times its scale as a pair of 16-bit values: off by less than 2^-20 of it, and by up to
+ * The products with V take a token's weight times its scale as a pair of 16-bit values: off by at most 2^-22 of it, and by up to
  * 2^-29 of the row's largest weight times its largest scale, which smaller products lose.  Both products' sums are cut off, not rounded, to
  * binary32 or a little less.  Values of bfloat16 queries below 2^-29 of their row's largest may be rounded, to a multiple of at most
  * 2^-38 of it.

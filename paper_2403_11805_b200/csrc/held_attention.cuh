@@ -446,7 +446,6 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
         int left = 0, odd_first = 0, odd_last = 0;            // tiles of the item in this run; what `left` is at its first and last tile if
                                                               // those may hold places nobody sees or the newest token (else -1)
         const float middle = kTwin && (lane & 2) ? 0.0f : -kMiddle / kUnit;                // of the columns of whole weights
-        const uint32_t cut = lane & 2 ? 0xffffe000u : 0u;     // keeps what fp16 holds of a weight
         bool begins = true, started = false;                  // the item's first tile here is next; the item has had a tile
 
         // a group of copies per trip (an empty one behind the last tile); the first trips only ask
@@ -752,10 +751,14 @@ __global__ void __launch_bounds__((ITEM ? HeldParts<S>::kWarps : kRunWarps) * 32
                                 w_sum[nt][grp][i] += p[i];
                             }
                             if constexpr (kTwin) {
-                                // the first four columns get the weights cut off to fp16, the others what was cut off
+                                // the first four columns get the weights cut off to fp16, the others what was cut off, to nearest (cut off
+                                // again it would be too small on average, which adds up over the tokens)
 #pragma unroll
-                                for (int i = 0; i < NC; ++i) p[i] -= __uint_as_float(__float_as_uint(p[i]) & cut);
-                                p_hi[nt][hh] = transpose8x8(pack_cut<false>(p[0], p[NC - 1]));
+                                for (int i = 0; i < NC; ++i) {
+                                    const float hi = __uint_as_float(__float_as_uint(p[i]) & 0xffffe000u);
+                                    p[i] = lane & 2 ? p[i] - hi : hi;
+                                }
+                                p_hi[nt][hh] = transpose8x8(pack_round<false>(p[0], p[NC - 1]));
                             } else {
                                 const uint32_t hi = pack_round<false>(p[0], p[1]);
                                 const float2 back = unpack<false>(hi);
