@@ -79,6 +79,15 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// (lo, hi) as a pair of 16-bit values, lo in the low half, cut off towards zero
+template <bool BF>
+__device__ __forceinline__ uint32_t pack_cut(float lo, float hi)
+{
+    uint32_t r;
+    if constexpr (BF) asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 template <int DB> struct DecodeShape : DecodeCols<DB> {
     static constexpr int kStages = DB == 1 ? 4 : 2;
     static constexpr int kHalf = DB * kTile * 128;            // K (or V) of a tile

@@ -96,15 +96,7 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// (lo, hi) as a pair of 16-bit values, lo in the low half; cut off towards zero or rounded to nearest
-template <bool BF>
-__device__ __forceinline__ uint32_t pack_cut(float lo, float hi)
-{
-    uint32_t r;
-    if constexpr (BF) asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
+// (lo, hi) as a pair of 16-bit values, lo in the low half, each rounded to nearest
 template <bool BF>
 __device__ __forceinline__ uint32_t pack_round(float lo, float hi)
 {
